@@ -320,6 +320,101 @@ aet_status aet_round_no_alloc(const aet_config* cfg, uint32_t client, uint32_t r
                               const float* w_in, float* U_out, float* w_out,
                               void* cuda_stream);
 
+/* ---- layers --------------------------------------------------------------- *
+ * The operators a model of this library is made of, on the caller's own device
+ * buffers: a dense layer (W as the models keep it, row-major [in, out]) with its
+ * gradient, the classification loss with its gradient, and dropout.  They are
+ * what aet_evaluate runs on; a program calls them itself for models, minibatches
+ * or losses of its own (Eq. 1 leaves f(w; xi) open).  No handle: all pointers are
+ * device pointers, every call is asynchronous on `cuda_stream`, allocates nothing,
+ * launches what it does on the caller's stream alone and can be captured into a
+ * CUDA graph.  Matrices are row-major, their rows `ld` elements apart (0: as many
+ * as there are columns), from an address that is a multiple of the element size.
+ * Sums, activations and statistics are held in fp32; a value is rounded to the
+ * element type (to nearest even) where it is stored.  The same call gives the same
+ * bits.  Errors: AET_ERR_ARG, AET_ERR_CUDA; text by aet_last_error(NULL).  */
+typedef enum { AET_F32 = 0, AET_BF16 = 1, AET_F16 = 2 } aet_dtype;
+typedef enum {
+  AET_ACT_NONE = 0,
+  AET_ACT_RELU = 1, /* derivative 0 at 0 */
+  AET_ACT_GELU = 2, /* z Phi(z), Phi by the error function */
+  AET_ACT_SILU = 3  /* z / (1 + exp(-z)) */
+} aet_act;
+
+/* Dropout with a mask that is a function of where an element stands and is never
+ * stored: element (r, c) of an array with C columns takes bits 16 (c mod 4) to
+ * 16 (c mod 4) + 15 of draw number counter + r * ceil(C / 4) + c / 4 of stream
+ * (seed, 4, client), the generator of every random quantity here (see
+ * aet_debug_draw).  It is dropped (0, whatever it was) if they are below
+ * q = round(65536 rate), and multiplied by 65536 / (65536 - q) otherwise.  A call
+ * on R rows uses up R * ceil(C / 4) draws: advance `counter` by that for other
+ * masks.  rate 0: nothing is dropped. */
+typedef struct {
+  uint64_t seed, counter;
+  uint32_t client;
+  float rate; /* 0 <= rate, q < 65536 */
+} aet_dropout_spec;
+
+/* y = residual + dropout(x): `rows` by `cols`, all of type dtype; residual may be
+ * null.  The gradient by x is the same call on dy without a residual.  y may be x
+ * or the residual (same address and ld), but not overlap them otherwise. */
+aet_status aet_dropout(uint32_t dtype, size_t rows, uint32_t cols, const aet_dropout_spec* drop,
+                       const void* x, size_t ld_x, const void* residual, size_t ld_residual, void* y,
+                       size_t ld_y, void* cuda_stream);
+
+/* Softmax cross-entropy of `rows` logit rows z with labels:
+ *   loss[r]    = log(sum_j exp(z_j)) - z_label                     (fp32)
+ *   dlogits[r] = scale * weight[r] * (softmax(z) - 1_label)        (dtype)
+ *   top[r]     = the lowest index of the row's maximum
+ * loss, dlogits, top and weight (1 each) may be null; dlogits may be the logits
+ * (same ld).  A negative label means a row without an answer: loss and gradient 0,
+ * top -1, whatever its logits hold.  -inf logits are classes that cannot be.  A row
+ * that holds NaN or +inf, or -inf only, or whose label is >= classes, has loss and
+ * gradient NaN; top is -1 where the row holds a NaN. */
+aet_status aet_cross_entropy(uint32_t dtype, size_t rows, uint32_t classes, const void* logits, size_t ld,
+                             const int32_t* labels, const float* weight, float scale, float* loss,
+                             void* dlogits, size_t ld_dlogits, int32_t* top, void* cuda_stream);
+
+/* A dense layer y = residual + dropout(act(z)), z = x W + b: x [rows, n_in],
+ * W [n_in, n_out], b [n_out], everything else [rows, n_out], all of type dtype.
+ * Plain data; struct_size = sizeof(aet_dense_desc). */
+typedef struct {
+  uint32_t struct_size;
+  uint32_t dtype, act; /* aet_dtype, aet_act */
+  uint32_t n_in, n_out;
+  uint32_t flags; /* AET_DENSE_* bits */
+  uint64_t ld_x, ld_w, ld_y, ld_residual, ld_pre, ld_dy, ld_dx, ld_dw; /* 0: no gaps */
+  aet_dropout_spec drop;
+} aet_dense_desc;
+
+/* x, W and dy may start at any element.  Without it they have to start on a
+ * 16-byte boundary (their rows need not), and the workspace is smaller. */
+#define AET_DENSE_ANY_ADDRESS 1u
+/* The backward pass adds to dW and db instead of writing them. */
+#define AET_DENSE_ACCUMULATE 2u
+
+/* Bytes of workspace a forward (backward 0) or backward (1) call on `rows` rows
+ * needs: device memory from a 256-byte boundary on, whose contents mean nothing
+ * before or after.  Calls that could overlap on the GPU (two streams, two captured
+ * graphs) need one each. */
+aet_status aet_dense_workspace(const aet_dense_desc* d, size_t rows, int backward, size_t* bytes);
+
+/* Forward.  bias, residual and pre may be null; pre receives z for the backward
+ * pass.  y may be the residual (same ld); otherwise outputs overlap nothing.  fp32
+ * operands are multiplied as three bf16 parts each (24 bits, fp32 sums); a row or
+ * column of operands that holds an infinity or NaN gives non-finite sums. */
+aet_status aet_dense_forward(const aet_dense_desc* d, size_t rows, const void* x, const void* w,
+                             const void* bias, const void* residual, void* y, void* pre, void* workspace,
+                             size_t workspace_bytes, void* cuda_stream);
+
+/* Gradient: dz = dropout(dy) act'(pre), dx = dz W^T, dW = x^T dz, db = sum of dz over
+ * the rows.  dx, dw, db may be null, x if dw is, w if dx is, pre if act is
+ * AET_ACT_NONE.  The residual's gradient is dy itself.  dz enters the two products
+ * rounded to dtype.  Outputs overlap nothing. */
+aet_status aet_dense_backward(const aet_dense_desc* d, size_t rows, const void* x, const void* w,
+                              const void* pre, const void* dy, void* dx, void* dw, void* db, void* workspace,
+                              size_t workspace_bytes, void* cuda_stream);
+
 /* ---- host-only helpers (no GPU needed) -------------------------------- */
 
 /* The integer schedule alone: what aet_run_rounds(n_rounds) on a fresh handle
@@ -333,7 +428,7 @@ aet_status aet_schedule_only(const aet_config* cfg, uint32_t n_rounds, aet_event
 uint32_t aet_debug_regression_kernel(uint32_t n_tasks, uint32_t longest, uint32_t by_value, const uint32_t* at_once);
 
 /* Draw number `counter` of stream (seed, stream, client); streams: 0 sample
- * index, 1 compute delay, 2 network delay. */
+ * index, 1 compute delay, 2 network delay, 3 the Setup split, 4 dropout. */
 uint64_t aet_debug_draw(uint64_t seed, uint32_t stream, uint32_t client, uint64_t counter);
 /* Delay in ticks from a 64-bit draw: dist 0 -> exponential with mean p0 ticks,
  * dist 1 -> uniform on [p0, p1] ticks. */

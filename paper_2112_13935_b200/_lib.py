@@ -51,6 +51,16 @@ class AetStats(C.Structure):
                 ("plan_ms", C.c_double)]
 
 
+class AetDropoutSpec(C.Structure):
+    _fields_ = [("seed", C.c_uint64), ("counter", C.c_uint64), ("client", C.c_uint32), ("rate", C.c_float)]
+
+
+class AetDenseDesc(C.Structure):
+    _fields_ = ([(n, C.c_uint32) for n in ("struct_size", "dtype", "act", "n_in", "n_out", "flags")]
+                + [(n, C.c_uint64) for n in ("ld_x", "ld_w", "ld_y", "ld_residual", "ld_pre", "ld_dy", "ld_dx", "ld_dw")]
+                + [("drop", AetDropoutSpec)])
+
+
 # name -> (restype, argtypes); every symbol include/aet.h declares
 PROTOTYPES = {
     "aet_create": (C.c_int, [C.POINTER(AetConfig), C.POINTER(C.c_void_p)]),
@@ -77,6 +87,13 @@ PROTOTYPES = {
     "aet_last_error": (C.c_char_p, [C.c_void_p]),
     "aet_round_no_alloc": (C.c_int, [C.POINTER(AetConfig), C.c_uint32, C.c_uint32, C.c_void_p, C.c_void_p,
                                      C.c_uint32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "aet_dropout": (C.c_int, [C.c_uint32, C.c_size_t, C.c_uint32, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p, C.c_size_t,
+                              C.c_void_p, C.c_size_t, C.c_void_p]),
+    "aet_cross_entropy": (C.c_int, [C.c_uint32, C.c_size_t, C.c_uint32, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p, C.c_float,
+                                    C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]),
+    "aet_dense_workspace": (C.c_int, [C.c_void_p, C.c_size_t, C.c_int, C.c_void_p]),
+    "aet_dense_forward": (C.c_int, [C.c_void_p, C.c_size_t] + [C.c_void_p] * 7 + [C.c_size_t, C.c_void_p]),
+    "aet_dense_backward": (C.c_int, [C.c_void_p, C.c_size_t] + [C.c_void_p] * 8 + [C.c_size_t, C.c_void_p]),
     "aet_schedule_only": (C.c_int, [C.POINTER(AetConfig), C.c_uint32, C.POINTER(AetEvent), C.c_size_t,
                                     C.POINTER(C.c_size_t), C.POINTER(AetSummary)]),
     "aet_debug_regression_kernel": (C.c_uint32, [C.c_uint32, C.c_uint32, C.c_uint32, C.POINTER(C.c_uint32)]),

@@ -244,6 +244,146 @@ def aet_debug_plan_layout(cfg, n_rounds) -> dict:
     return out
 
 
+# ---- layers: torch tensors on the current CUDA device ----------------------------------------------------------------------
+
+ACTS = dict(none=0, relu=1, gelu=2, silu=3)           # AET_ACT_*
+DENSE_ANY_ADDRESS, DENSE_ACCUMULATE = 1, 2            # AET_DENSE_*
+_dtypes = {}
+
+
+def _dtype(t) -> int:
+    """AET_F32, AET_BF16 or AET_F16 of a torch dtype."""
+    if not _dtypes:
+        import torch
+        _dtypes.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+    if t not in _dtypes:
+        raise AetError(1, f"element type {t} is not float32, bfloat16 or float16")
+    return _dtypes[t]
+
+
+def _here(device) -> int:
+    """The current stream of the current device, which the tensors have to be on."""
+    import torch
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        raise AetError(1, f"tensors have to be on the current CUDA device, not on {device}")
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _raw_stream(t, stream) -> int:
+    here = _here(t.device)
+    return here if stream is None else stream if isinstance(stream, int) else stream.cuda_stream
+
+
+def _at(t, like, shape, what, ld=None):
+    """Address of a matrix or vector of `like`'s type and device (None: null)."""
+    if t is None:
+        return None
+    if t.dtype is not like.dtype or t.device != like.device or t.shape != shape:
+        raise AetError(1, f"{what}: {tuple(t.shape)} of {t.dtype} on {t.device}, expected {tuple(shape)} of {like.dtype} on {like.device}")
+    strides = t.stride()
+    if t.numel() and ((shape[-1] > 1 and strides[-1] != 1) or (ld is not None and shape[0] > 1 and strides[0] != ld)):
+        raise AetError(1, f"{what}: strides {strides}, expected rows {ld} elements apart of neighbouring elements")
+    return t.data_ptr()
+
+
+def _ld(t) -> int:
+    """Elements between the rows of a matrix."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def aet_dropout_spec(seed: int, client: int = 0, counter: int = 0, rate: float = 0.0):
+    return _lib.AetDropoutSpec(seed=seed, client=client, counter=counter, rate=rate)
+
+
+def aet_dropout(drop, x, y, residual=None, stream=None):
+    """y = residual + dropout(x); see include/aet.h for which elements a (seed, client, counter) drops."""
+    shape = x.shape
+    if len(shape) != 2:
+        raise AetError(1, "x: a matrix is expected")
+    _check(None, _lib.load().aet_dropout(
+        _dtype(x.dtype), shape[0], shape[1], C.addressof(drop), _at(x, x, shape, "x"), _ld(x),
+        _at(residual, x, shape, "residual"), 0 if residual is None else _ld(residual), _at(y, x, shape, "y"), _ld(y), _raw_stream(x, stream)))
+
+
+def aet_cross_entropy(logits, labels, loss=None, dlogits=None, top=None, weight=None, scale: float = 1.0, stream=None):
+    """Softmax cross-entropy of each row, its gradient times `scale` (and `weight`), and the lowest index of its maximum."""
+    import torch
+    shape = logits.shape
+    if len(shape) != 2:
+        raise AetError(1, "logits: a matrix is expected")
+    for t, kind, what in ((labels, torch.int32, "labels"), (loss, torch.float32, "loss"), (top, torch.int32, "top"), (weight, torch.float32, "weight")):
+        if t is not None and (t.dtype is not kind or t.shape != shape[:1] or not t.is_contiguous() or t.device != logits.device):
+            raise AetError(1, f"{what}: {tuple(t.shape)} of {t.dtype} on {t.device}, expected {shape[0]} neighbouring {kind} on {logits.device}")
+    p = lambda t: None if t is None else t.data_ptr()   # noqa: E731
+    _check(None, _lib.load().aet_cross_entropy(
+        _dtype(logits.dtype), shape[0], shape[1], _at(logits, logits, shape, "logits"), _ld(logits), p(labels), p(weight), scale, p(loss),
+        _at(dlogits, logits, shape, "dlogits"), 0 if dlogits is None else _ld(dlogits), p(top), _raw_stream(logits, stream)))
+
+
+def aet_dense(n_in: int, n_out: int, dtype=None, act: str = "none", dropout=None, ld_in: int = 0, ld_out: int = 0, ld_w: int = 0, flags: int = 0, **lds):
+    """Descriptor of a dense layer.  dtype: a torch dtype (float32).  ld_in: rows of x and dx, ld_out: of y, residual, pre and dy,
+    ld_w: of W and dW; ld_x=, ld_dw= and so on for one alone; 0: no gaps."""
+    d = _lib.AetDenseDesc()
+    d.struct_size = C.sizeof(_lib.AetDenseDesc)
+    d.dtype = 0 if dtype is None else _dtype(dtype)
+    if act not in ACTS:
+        raise AetError(1, f"activation {act!r} is not one of {', '.join(ACTS)}")
+    d.act, d.n_in, d.n_out, d.flags = ACTS[act], n_in, n_out, flags
+    d.ld_x = d.ld_dx = ld_in or n_in
+    d.ld_w = d.ld_dw = ld_w or n_out
+    d.ld_y = d.ld_residual = d.ld_pre = d.ld_dy = ld_out or n_out
+    for k, v in lds.items():
+        if not k.startswith("ld_") or not hasattr(d, k):
+            raise AetError(1, f"unknown argument {k}")
+        setattr(d, k, v or (n_in if k in ("ld_x", "ld_dx") else n_out))
+    if dropout is not None:
+        d.drop = dropout
+    return d
+
+
+def aet_dense_workspace(d, rows: int, backward: bool = False) -> int:
+    """Bytes of workspace a call on so many rows needs."""
+    n = C.c_size_t()
+    _check(None, _lib.load().aet_dense_workspace(C.addressof(d), rows, int(backward), C.addressof(n)))
+    return int(n.value)
+
+
+def _space(workspace, like):
+    if workspace is None:
+        return None, 0
+    if workspace.device != like.device or not workspace.is_contiguous():
+        raise AetError(1, "workspace: a contiguous tensor on the layer's device is expected")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _rows_of(d, x, cols, what):
+    if len(x.shape) != 2 or x.shape[1] != cols or _dtype(x.dtype) != d.dtype:
+        raise AetError(1, f"{what}: {tuple(x.shape)} of {x.dtype} does not fit the descriptor")
+    return x.shape[0]
+
+
+def aet_dense_forward(d, x, w, bias, y, residual=None, pre=None, workspace=None, stream=None):
+    """y = residual + dropout(act(x w + bias)); pre: where x w + bias goes for the backward pass."""
+    rows, n_in, n_out = _rows_of(d, x, d.n_in, "x"), d.n_in, d.n_out
+    out = (rows, n_out)
+    ws, size = _space(workspace, x)
+    _check(None, _lib.load().aet_dense_forward(
+        C.addressof(d), rows, _at(x, x, (rows, n_in), "x", d.ld_x), _at(w, x, (n_in, n_out), "w", d.ld_w), _at(bias, x, (n_out,), "bias"),
+        _at(residual, x, out, "residual", d.ld_residual), _at(y, x, out, "y", d.ld_y), _at(pre, x, out, "pre", d.ld_pre), ws, size,
+        _raw_stream(x, stream)))
+
+
+def aet_dense_backward(d, x, w, dy, pre=None, dx=None, dw=None, db=None, workspace=None, stream=None):
+    """dx, dw and db (any of them None) of the layer from dy."""
+    rows, n_in, n_out = _rows_of(d, dy, d.n_out, "dy"), d.n_in, d.n_out
+    out = (rows, n_out)
+    ws, size = _space(workspace, dy)
+    _check(None, _lib.load().aet_dense_backward(
+        C.addressof(d), rows, _at(x, dy, (rows, n_in), "x", d.ld_x), _at(w, dy, (n_in, n_out), "w", d.ld_w), _at(pre, dy, out, "pre", d.ld_pre),
+        _at(dy, dy, out, "dy", d.ld_dy), _at(dx, dy, (rows, n_in), "dx", d.ld_dx), _at(dw, dy, (n_in, n_out), "dw", d.ld_dw),
+        _at(db, dy, (n_out,), "db"), ws, size, _raw_stream(dy, stream)))
+
+
 class Session:
     """Convenience wrapper: create, load every client's data, run, read back."""
 

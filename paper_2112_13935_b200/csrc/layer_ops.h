@@ -1,0 +1,77 @@
+// Launch interfaces of the layer operators (dense layer, classification loss, dropout): plain structs, no library types.
+#pragma once
+#include <cuda_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace aet {
+namespace layer {
+
+enum DType : uint32_t { kF32 = 0, kBf16 = 1, kF16 = 2 };
+enum Act : uint32_t { kNone = 0, kRelu = 1, kGelu = 2, kSilu = 3 };
+inline size_t type_bytes(uint32_t t) { return t == kF32 ? 4 : 2; }
+
+// Dropout of an array of rows: draw counter + row * ceil(cols / 4) + col / 4 of the key's stream holds sixteen bits for each of
+// four neighbouring elements; one whose bits are below q of 65,536 is dropped, the others are multiplied by `scale`.
+struct Drop {
+  uint64_t key, counter;
+  uint32_t q;        // 0: nothing is dropped
+  float scale;       // 65536 / (65536 - q)
+};
+
+// What becomes of four neighbouring sums z = (A B)[row, col .. col + 3] of a product: pre = z + bias,
+// out = residual + drop(act(pre)).
+struct Epilogue {
+  const void* bias;      // [cols] or null
+  const void* residual;  // [rows, ld_res] of the outputs' type, or null; may be `out` itself
+  void* out;             // [rows, ld_out]
+  void* pre;             // [rows, ld_pre] of the outputs' type, or null
+  size_t ld_res, ld_out, ld_pre;
+  uint32_t bias_type, out_type, act;
+  uint32_t vec;          // out, pre and residual can be touched four columns at a time
+  Drop drop;
+};
+
+// C [m, n] = A B through the epilogue: A(i, k) = a[i a_row + k a_col], B(k, j) = b[k b_row + j b_col], elements of `type`.
+struct Product {
+  const void *a, *b;
+  size_t a_row, a_col, b_row, b_col;
+  uint32_t type;
+  uint32_t m, n, k;
+  Epilogue e;
+};
+
+// Small products: 64 x 64 tiles on FMAs, k split over the CTAs of a cluster.
+cudaError_t launch_product_fma(const Product& p, cudaStream_t s);
+
+// dz = drop(dy) act'(pre), to `dz` (null: not kept), and its sums over the rows to db.
+struct SlopeLaunch {
+  const void *dy, *pre;   // pre null: act is none
+  void *dz, *db;          // db null: no sums
+  size_t ld_dy, ld_pre, ld_dz;
+  uint32_t type, db_type, act, accumulate;   // accumulate: db += sums
+  uint32_t rows, cols;
+  Drop drop;
+  float* partial;         // slope_partial_floats() of workspace
+};
+size_t slope_partial_floats(uint32_t rows, uint32_t cols);
+cudaError_t launch_slope(const SlopeLaunch& p, cudaStream_t s);
+
+cudaError_t launch_dropout(uint32_t type, size_t rows, uint32_t cols, const Drop& d, const void* x, size_t ld_x, const void* residual,
+                           size_t ld_res, void* y, size_t ld_y, cudaStream_t s);
+
+struct LossLaunch {
+  const void* logits;
+  const int32_t* labels;
+  const float* weight;    // [rows] or null
+  float* loss;            // [rows] or null
+  void* grad;             // [rows, ld_grad] of the logits' type, or null; may be the logits
+  int32_t* top;           // [rows] or null
+  size_t ld, ld_grad, rows;
+  uint32_t type, classes;
+  float scale;
+};
+cudaError_t launch_loss(const LossLaunch& p, cudaStream_t s);
+
+}  // namespace layer
+}  // namespace aet

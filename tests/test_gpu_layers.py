@@ -1,0 +1,399 @@
+"""Layer operators against plain 64-bit forms: every type, odd sizes, gaps between rows, odd addresses, each option."""
+import numpy as np
+import pytest
+import torch
+
+import layer_helpers as lh
+from paper_2112_13935_b200 import api
+
+pytestmark = pytest.mark.gpu
+
+STEP = 2.0 ** -23
+
+
+def layer_inputs(rows, n_in, n_out, dtype, seed):
+    r = np.random.default_rng(seed)
+    q = lambda a: torch.as_tensor(a).to(dtype).double().numpy()   # noqa: E731  the values the type holds
+    return dict(x=q(np.maximum(r.standard_normal((rows, n_in)), 0)), w=q(r.uniform(-1, 1, (n_in, n_out)) * (3 / n_in) ** 0.5),
+                bias=q(r.standard_normal(n_out) * 0.1), residual=q(r.standard_normal((rows, n_out))), dy=q(r.standard_normal((rows, n_out))),
+                pre=q(r.standard_normal((rows, n_out))))
+
+
+def workspace(plan, rows, backward):
+    n = api.aet_dense_workspace(plan, rows, backward)
+    return torch.full((n + 256,), 0xFF, dtype=torch.uint8, device="cuda")[:n]     # (NaN in every type)
+
+
+def check_forward(rows, n_in, n_out, type, act="none", bias=True, residual=False, pre=False, rate=0.0, pad=0, shift=0, seed=1, in_place=False):
+    t = lh.TYPES[type]
+    d = layer_inputs(rows, n_in, n_out, t, seed)
+    drop = api.aet_dropout_spec(seed=seed, client=3, counter=2 ** 40 + 5, rate=rate)
+    plan = api.aet_dense(n_in, n_out, dtype=t, act=act, dropout=drop, ld_in=n_in + pad, ld_out=n_out + pad, ld_w=n_out + pad,
+                         flags=api.DENSE_ANY_ADDRESS if shift else 0)
+    x, _ = lh.matrix(d["x"], t, pad, shift)
+    w, _ = lh.matrix(d["w"], t, pad, shift)
+    b = torch.as_tensor(d["bias"]).to(t).cuda() if bias else None
+    res = lh.matrix(d["residual"], t, pad, shift) if residual else (None, None)
+    y, ybuf = res if in_place else lh.matrix(np.zeros((rows, n_out)), t, pad, shift)
+    z, zbuf = lh.matrix(np.zeros((rows, n_out)), t, pad, shift) if pre else (None, None)
+    api.aet_dense_forward(plan, x, w, b, y, residual=res[0], pre=z, workspace=workspace(plan, rows, False))
+    torch.cuda.synchronize()
+    size = np.abs(d["x"]) @ np.abs(d["w"]) + (np.abs(d["bias"]) if bias else 0)
+    slack = (n_in + 16) * STEP * size
+    want = d["x"] @ d["w"] + (d["bias"] if bias else 0)
+    if pre:
+        lh.assert_close(z, want, t, slack, "pre")
+        assert lh.gaps_untouched(z, zbuf, pad, shift)
+    # the activations' slopes stay below 1.13 and their own error below four steps of their argument's magnitude
+    want, slack = lh.act(want, act), 1.13 * slack + 4 * STEP * size
+    if rate:
+        mask, factor = lh.kept(rows, n_out, seed, 3, 2 ** 40 + 5, rate)
+        want, slack = np.where(mask, want * factor, 0), np.where(mask, slack * factor + 2 * STEP * np.abs(want * factor), 0)
+    if residual:
+        want, slack = want + d["residual"], slack + STEP * (np.abs(want) + np.abs(d["residual"]))
+    lh.assert_close(y, want, t, slack, "y")
+    assert lh.gaps_untouched(y, ybuf, pad, shift)
+
+
+SHAPES = [(1, 1, 1), (1, 7, 3), (2, 64, 64), (5, 65, 130), (33, 784, 10), (64, 100, 37), (65, 785, 128), (130, 33, 257), (300, 256, 65)]
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,n_in,n_out", SHAPES)
+def test_dense_forward_sizes(rows, n_in, n_out, type):
+    check_forward(rows, n_in, n_out, type, act="relu", pre=True)
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("over", [
+    dict(act="none", bias=False), dict(act="gelu", residual=True), dict(act="silu", rate=0.3), dict(act="relu", rate=0.5, residual=True, pre=True),
+    dict(pad=1, act="gelu", residual=True, pre=True), dict(pad=3, shift=1, rate=0.1, residual=True, pre=True), dict(pad=8, act="silu"),
+    dict(residual=True, in_place=True, act="relu"), dict(rate=0.9999), dict(rate=2.0 ** -18)])
+def test_dense_forward_options(type, over):
+    check_forward(70, 131, 94, type, **over)
+
+
+def check_backward(rows, n_in, n_out, type, act="none", rate=0.0, pad=0, shift=0, accumulate=False, want=("dx", "dw", "db"), seed=2):
+    t = lh.TYPES[type]
+    d = layer_inputs(rows, n_in, n_out, t, seed)
+    drop = api.aet_dropout_spec(seed=seed, client=0, counter=9, rate=rate)
+    flags = (api.DENSE_ANY_ADDRESS if shift else 0) | (api.DENSE_ACCUMULATE if accumulate else 0)
+    plan = api.aet_dense(n_in, n_out, dtype=t, act=act, dropout=drop, ld_in=n_in + pad, ld_out=n_out + pad, ld_w=n_out + pad, flags=flags)
+    at = {k: lh.matrix(d[k], t, pad, shift)[0] for k in ("x", "w", "dy", "pre")}
+    before = dict(dx=np.zeros((rows, n_in)), dw=d["w"] * 3, db=d["bias"][None])
+    before = {k: torch.as_tensor(v).to(t).double().numpy() for k, v in before.items()}
+    out = {k: lh.matrix(before[k], t, 0 if k == "db" else pad, shift) for k in want}
+    args = {k: (v[0][0] if k == "db" else v[0]) for k, v in out.items()}
+    api.aet_dense_backward(plan, at["x"] if "dw" in want else None, at["w"] if "dx" in want else None, at["dy"],
+                           pre=None if act == "none" else at["pre"], workspace=workspace(plan, rows, True), **args)
+    torch.cuda.synchronize()
+    dz = d["dy"] * lh.slope(d["pre"], act)
+    off = 8 * STEP * np.abs(d["dy"])              # the slopes are below 1.13, and off by a few steps
+    if rate:
+        mask, factor = lh.kept(rows, n_out, seed, 0, 9, rate)
+        dz, off = np.where(mask, dz * factor, 0), np.where(mask, off * factor + 2 * STEP * np.abs(dz * factor), 0)
+    in_type = off + (0 if act == "none" and not rate else lh.HALF_STEP[t] * np.abs(dz) + lh.TINY[t])   # dz as the products take it
+    plus = {k: before[k] if accumulate and k != "dx" else 0 for k in before}
+    if "dx" in want:
+        size = np.abs(dz) @ np.abs(d["w"]).T
+        lh.assert_close(out["dx"][0], dz @ d["w"].T, t, in_type @ np.abs(d["w"]).T + (n_out + 16) * STEP * size, "dx")
+    if "dw" in want:
+        size = np.abs(d["x"]).T @ np.abs(dz) + np.abs(plus["dw"])
+        lh.assert_close(out["dw"][0], d["x"].T @ dz + plus["dw"], t, np.abs(d["x"]).T @ in_type + (rows + 16) * STEP * size, "dw")
+    if "db" in want:
+        size = np.abs(dz).sum(0)[None] + np.abs(plus["db"])
+        lh.assert_close(out["db"][0], dz.sum(0)[None] + plus["db"], t, off.sum(0)[None] + (rows + 16) * STEP * size, "db")
+    for k, (m, buf) in out.items():
+        assert lh.gaps_untouched(m, buf, 0 if k == "db" else pad, shift), k
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,n_in,n_out", SHAPES)
+def test_dense_backward_sizes(rows, n_in, n_out, type):
+    check_backward(rows, n_in, n_out, type, act="relu")
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("over", [
+    dict(), dict(act="gelu"), dict(act="silu", rate=0.3), dict(act="relu", rate=0.5, pad=1), dict(act="gelu", pad=3, shift=1),
+    dict(act="relu", accumulate=True, pad=8), dict(accumulate=True), dict(want=("dw",)), dict(want=("dx",), act="silu"), dict(want=("db",), act="relu"),
+    dict(want=("dw", "db"), rate=0.2)])
+def test_dense_backward_options(type, over):
+    check_backward(90, 77, 139, type, **over)
+
+
+def test_dense_backward_over_no_rows_is_zero():
+    plan = api.aet_dense(5, 3, ld_w=4)
+    dw, buf = lh.matrix(np.ones((5, 3)), torch.float32, 1)
+    db = torch.ones(3, device="cuda")
+    empty = lambda n: torch.empty(0, n, device="cuda")   # noqa: E731
+    w, _ = lh.matrix(np.ones((5, 3)), torch.float32, 1)
+    api.aet_dense_backward(plan, empty(5), w, empty(3), dx=empty(5), dw=dw, db=db)
+    api.aet_dense_forward(plan, empty(5), w, None, empty(3))
+    torch.cuda.synchronize()
+    assert not dw.any() and not db.any() and lh.gaps_untouched(dw, buf, 1, 0)
+
+
+def test_dense_gradient_agrees_with_differences():
+    """fp32 forward passes at both sides of a step against the backward pass: F = sum of dy * y."""
+    rows, n_in, n_out = 9, 20, 14
+    d = layer_inputs(rows, n_in, n_out, torch.float32, 5)
+    c = {k: torch.as_tensor(v).float().cuda() for k, v in d.items()}
+    plan = api.aet_dense(n_in, n_out, act="silu", dropout=api.aet_dropout_spec(seed=1, rate=0.25))
+    y, pre = torch.empty(rows, n_out, device="cuda"), torch.empty(rows, n_out, device="cuda")
+
+    def F(x, w, b):
+        api.aet_dense_forward(plan, x, w, b, y, pre=pre)
+        return float((y.double() * c["dy"].double()).sum())
+
+    F(c["x"], c["w"], c["bias"])
+    g = dict(dx=torch.empty_like(c["x"]), dw=torch.empty_like(c["w"]), db=torch.empty_like(c["bias"]))
+    api.aet_dense_backward(plan, c["x"], c["w"], c["dy"], pre=pre, workspace=workspace(plan, rows, True), **g)
+    # a step of 2^-6: the third derivative of silu stays below 0.31 and |x|, |w| below 4, so the difference quotient is off by at most
+    # 2^-12 / 6 * 0.31 * 64 * sum |dy| factor < 0.002 sum |dy|; fp32 rounding adds 2^-20 sum |y dy| * 2^6
+    h = 2.0 ** -6
+    for k, name in enumerate(("x", "w", "bias")):
+        for at in [(0,), (3,)] if name == "bias" else [(0, 0), (4, 7), (8, 13)]:
+            side = []
+            for sign in (1, -1):
+                v = [c["x"].clone(), c["w"].clone(), c["bias"].clone()]
+                v[k][at] += sign * h
+                side.append(F(*v))
+            got = float(g["d" + {"x": "x", "w": "w", "bias": "b"}[name]][at])
+            assert abs((side[0] - side[1]) / (2 * h) - got) <= 0.003 * float(c["dy"].abs().sum()) / n_out + 2.0 ** -13, (name, at)
+
+
+# ---- loss ----------------------------------------------------------------------------------------------------------------
+
+def loss_reference(z, labels, scale, weight):
+    """loss, gradient and top in 64 bits, with the rules for rows that have none."""
+    rows, n = z.shape
+    loss, grad, top = np.zeros(rows), np.zeros((rows, n)), np.full(rows, -1)
+    for r in range(rows):
+        y = labels[r]
+        if y < 0:
+            continue
+        if not np.isnan(z[r]).any():
+            top[r] = int(np.argmax(z[r]))
+        m = z[r].max()
+        if np.isnan(z[r]).any() or np.isinf(m) or y >= n:
+            loss[r], grad[r] = np.nan, np.nan
+            continue
+        e = np.exp(z[r] - m)
+        with np.errstate(divide="ignore"):
+            loss[r] = np.log(e.sum()) + m - z[r, y]
+        grad[r] = e / e.sum()
+        grad[r, y] -= 1
+        grad[r] *= scale * (1 if weight is None else weight[r])
+    return loss, grad, top
+
+
+def check_loss(z, labels, type, scale=1.0, weight=None, pad=0, shift=0, in_place=False, outs=("loss", "dlogits", "top")):
+    t = lh.TYPES[type]
+    rows, n = z.shape
+    with np.errstate(invalid="ignore"):
+        z = torch.as_tensor(z).to(t).double().numpy()
+    logits, lbuf = lh.matrix(z, t, pad, shift)
+    y = torch.as_tensor(np.asarray(labels, dtype=np.int32)).cuda()
+    w = None if weight is None else torch.as_tensor(weight).float().cuda()
+    got = dict(loss=torch.full((rows,), 5.0, device="cuda"), top=torch.full((rows,), 5, dtype=torch.int32, device="cuda"))
+    got["dlogits"], gbuf = (logits, lbuf) if in_place else lh.matrix(np.ones((rows, n)), t, pad, shift)
+    api.aet_cross_entropy(logits, y, weight=w, scale=scale, **{k: got[k] for k in outs})
+    torch.cuda.synchronize()
+    want = dict(zip(("loss", "dlogits", "top"), loss_reference(z, labels, scale, None if weight is None else np.asarray(weight, np.float32).astype(float))))
+    # exp is off by 2^-22 of itself and the difference under it by 2^-24 of itself; adding n of them in any order by n 2^-24
+    spread = np.nan_to_num(np.where(np.isinf(z), 0, np.abs(z)).max(1), nan=0.0) * 2
+    rel = (n + 16) * 2.0 ** -24 + 2.0 ** -21 + spread * 2.0 ** -23
+    for k in outs:
+        if k == "top":
+            assert np.array_equal(got["top"].cpu().numpy(), want["top"])
+            continue
+        a, b = lh.host(got[k]), want[k]
+        assert np.array_equal(np.isnan(a), np.isnan(b)), k
+        assert np.array_equal(np.isinf(a), np.isinf(b)) and (a[np.isinf(b)] > 0).all(), k
+        fine = np.isfinite(b)
+        if k == "loss":
+            slack = rel + 2.0 ** -22 * (np.abs(np.where(fine, b, 0)) + spread)
+            off = np.abs(a[fine] - b[fine])
+            assert (off <= slack[fine]).all(), (off / slack[fine]).max()
+        else:
+            wgt = scale * (np.ones(rows) if weight is None else np.abs(weight))
+            with np.errstate(invalid="ignore"):
+                slack = (4 * rel * wgt)[:, None] * (np.abs(b) / np.maximum(wgt, 1e-300)[:, None]) + (2.0 ** -22 * wgt)[:, None] * (np.arange(n)[None] == np.asarray(labels)[:, None])
+            lh.assert_close(a[fine], b[fine], t, slack[fine], k)
+    if "dlogits" in outs:
+        assert lh.gaps_untouched(got["dlogits"], gbuf, pad, shift)
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,n", [(1, 1), (3, 2), (7, 10), (300, 10), (33, 31), (40, 33), (9, 100), (5, 257), (3, 1000), (2, 1025), (3, 4099), (2, 30001), (1, 131072)])
+def test_loss_sizes(rows, n, type):
+    r = np.random.default_rng(rows * 1000 + n)
+    z = r.standard_normal((rows, n)) * 2
+    labels = r.integers(0, n, rows)
+    labels[rows // 2] = -1 if rows > 2 else labels[rows // 2]
+    check_loss(z, labels, type, scale=1.0 / rows)
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("n", [10, 37, 700, 5003])
+@pytest.mark.parametrize("over", [dict(pad=1), dict(pad=3, shift=1), dict(pad=8), dict(in_place=True), dict(weighted=True), dict(outs=("loss",)),
+                                  dict(outs=("dlogits",)), dict(outs=("top",))])
+def test_loss_options(type, n, over):
+    r = np.random.default_rng(n)
+    over = dict(over)
+    if over.pop("weighted", False):
+        over["weight"] = r.uniform(0, 2, 12).astype(np.float32)
+    check_loss(r.standard_normal((12, n)), r.integers(-1, n, 12), type, scale=0.125, **over)
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("n", [2, 10, 70, 2500, 9001])
+def test_loss_of_odd_rows(n, type):
+    """Infinities, NaN, the type's lowest value, ties, labels that are none: every rule of the header."""
+    r = np.random.default_rng(7)
+    low = torch.finfo(lh.TYPES[type]).min
+    z = r.standard_normal((14, n))
+    labels = np.full(14, n - 1)
+    z[0, : n - 1] = -np.inf                     # one class left
+    z[1] = -np.inf                              # none left
+    z[2, 0] = np.inf
+    z[3, n // 2] = np.nan
+    z[4] = np.nan; labels[4] = -1               # not read
+    z[5] = low                                  # a mask of the lowest value that leaves nothing: uniform
+    z[6, : n - 1] = low
+    z[7] = 1.0                                  # ties: the first
+    labels[8] = n                               # no such class
+    labels[9] = -2 ** 31
+    z[10, n - 1] = -np.inf                      # the label itself cannot be: loss inf
+    z[11, 0] = -torch.finfo(lh.TYPES[type]).min / 2    # one class far above the rest
+    labels[11] = 0
+    z[12] = r.standard_normal(n) * 1e-3 + 500   # far from zero
+    z[13, 1] = np.nan
+    z[13, 0] = np.inf
+    check_loss(z, labels, type)
+
+
+# ---- dropout -------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 3), (3, 4), (5, 9), (129, 1001), (64, 64), (700, 128), (2, 70000)])
+@pytest.mark.parametrize("over", [dict(rate=0.5), dict(rate=0.1, residual=True), dict(rate=0.0), dict(rate=0.9999, pad=1, shift=1, residual=True), dict(rate=0.3, pad=4, in_place="x"), dict(rate=0.3, residual=True, in_place="residual")])
+def test_dropout(rows, cols, type, over):
+    t = lh.TYPES[type]
+    r = np.random.default_rng(cols)
+    q = lambda a: torch.as_tensor(a).to(t).double().numpy()   # noqa: E731
+    pad, shift, rate = over.get("pad", 0), over.get("shift", 0), over["rate"]
+    xv, rv = q(r.standard_normal((rows, cols))), q(r.standard_normal((rows, cols)))
+    if rate:
+        mask, factor = lh.kept(rows, cols, 11, 5, 2 ** 64 - 3, rate)    # (the counter wraps)
+        xv[~mask] = np.nan                                     # a dropped element is zero whatever it was
+    else:
+        mask, factor = np.ones((rows, cols), bool), 1.0
+    x, xbuf = lh.matrix(xv, t, pad, shift)
+    res, rbuf = lh.matrix(rv, t, pad, shift) if over.get("residual") else (None, None)
+    place = over.get("in_place")
+    y, ybuf = (x, xbuf) if place == "x" else (res, rbuf) if place else lh.matrix(np.zeros((rows, cols)), t, pad, shift)
+    api.aet_dropout(api.aet_dropout_spec(11, 5, 2 ** 64 - 3, rate), x, y, residual=res)
+    torch.cuda.synchronize()
+    want = np.where(mask, xv * factor, 0)
+    slack = 2 * STEP * np.abs(want)
+    if res is not None:
+        want, slack = want + rv, slack + STEP * (np.abs(want) + np.abs(rv))
+    lh.assert_close(y, want, t, slack)
+    assert lh.gaps_untouched(y, ybuf, pad, shift)
+
+
+def test_dropout_rate_is_what_was_asked():
+    """q of 65,536 in expectation; five standard deviations either way, and rows, columns and lanes alike."""
+    rows, cols = 512, 1024
+    y = torch.empty(rows, cols, device="cuda")
+    for rate in (0.1, 0.5, 0.75):
+        api.aet_dropout(api.aet_dropout_spec(3, rate=rate), torch.ones(rows, cols, device="cuda"), y)
+        gone = (y == 0).double()
+        for share, n in ((gone.mean(), rows * cols), (gone[:, ::4].mean(), rows * cols / 4), (gone[:, 3::4].mean(), rows * cols / 4)):
+            assert abs(float(share) - rate) <= 5 * (rate * (1 - rate) / n) ** 0.5 + 2.0 ** -17
+
+
+# ---- together, streams, graphs -------------------------------------------------------------------------------------------
+
+def training_step(c, plans, ws, out):
+    """Two layers, the loss, and all gradients."""
+    p1, p2 = plans
+    api.aet_dense_forward(p1, c["x"], c["w1"], c["b1"], out["h"], pre=out["z"], workspace=ws[0])
+    api.aet_dense_forward(p2, out["h"], c["w2"], c["b2"], out["logits"], workspace=ws[1])
+    api.aet_cross_entropy(out["logits"], c["labels"], loss=out["loss"], dlogits=out["g"], top=out["top"], scale=1 / c["x"].shape[0])
+    api.aet_dense_backward(p2, out["h"], c["w2"], out["g"], dx=out["gh"], dw=out["dw2"], db=out["db2"], workspace=ws[2])
+    api.aet_dense_backward(p1, c["x"], c["w1"], out["gh"], pre=out["z"], dw=out["dw1"], db=out["db1"], workspace=ws[3])
+
+
+def step_state(rows, dims, dtype, seed, rate):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    n0, n1, n2 = dims
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda")   # noqa: E731
+    c = dict(x=rnd(rows, n0).to(dtype), w1=(rnd(n0, n1) / n0 ** 0.5).to(dtype), b1=rnd(n1).to(dtype), w2=(rnd(n1, n2) / n1 ** 0.5).to(dtype),
+             b2=rnd(n2).to(dtype), labels=torch.randint(0, n2, (rows,), generator=g, device="cuda", dtype=torch.int32))
+    plans = (api.aet_dense(n0, n1, dtype=dtype, act="gelu", dropout=api.aet_dropout_spec(seed, rate=rate)), api.aet_dense(n1, n2, dtype=dtype))
+    ws = [torch.empty(api.aet_dense_workspace(p, rows, b), dtype=torch.uint8, device="cuda") for b in (False, True) for p in plans]
+    ws = [ws[0], ws[1], ws[3], ws[2]]
+    e = lambda *s: torch.empty(*s, dtype=dtype, device="cuda")   # noqa: E731
+    out = dict(h=e(rows, n1), z=e(rows, n1), logits=e(rows, n2), g=e(rows, n2), gh=e(rows, n1), dw1=e(n0, n1), db1=e(n1), dw2=e(n1, n2), db2=e(n2),
+               loss=torch.empty(rows, device="cuda"), top=torch.empty(rows, dtype=torch.int32, device="cuda"))
+    return c, plans, ws, out
+
+
+@pytest.mark.parametrize("rows,dims,rate", [(50, (100, 64, 10), 0.0), (257, (784, 130, 37), 0.2)])
+def test_a_training_step_against_autograd_in_64_bits(rows, dims, rate):
+    c, plans, ws, out = step_state(rows, dims, torch.float32, 4, rate)
+    training_step(c, plans, ws, out)
+    leaf = {k: c[k].double().requires_grad_() for k in ("w1", "b1", "w2", "b2")}
+    h = torch.nn.functional.gelu(c["x"].double() @ leaf["w1"] + leaf["b1"])
+    if rate:
+        mask, factor = lh.kept(rows, dims[1], 4, 0, 0, rate)
+        h = h * torch.as_tensor(mask).cuda() * factor
+    logits = h @ leaf["w2"] + leaf["b2"]
+    loss = torch.nn.functional.cross_entropy(logits, c["labels"].long(), reduction="none")
+    loss.mean().backward()
+    # fp32 sums of up to 784 terms twice on the way in and as many on the way back: some 1e-6, against the largest entry
+    for got, want in [(out["loss"], loss)] + [(out["d" + k], leaf[k].grad) for k in leaf]:
+        want = want.detach()
+        assert float((got.double() - want).abs().max() / want.abs().max()) <= 2e-5
+    assert torch.equal(out["top"].long(), out["logits"].argmax(1))
+
+
+def test_a_training_step_repeats_bit_for_bit_on_streams_and_in_graphs():
+    c, plans, ws, out = step_state(200, (300, 96, 33), torch.bfloat16, 8, 0.1)
+    training_step(c, plans, ws, out)
+    torch.cuda.synchronize()
+    first = {k: v.clone() for k, v in out.items()}
+    side = torch.cuda.Stream()
+    for v in out.values():
+        v.zero_()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        training_step(c, plans, ws, out)
+    side.synchronize()
+    assert all(torch.equal(first[k], out[k]) for k in out)
+    # two graphs of two states, each with its own workspaces, replayed at the same time
+    states = [(c, plans, ws, out), step_state(200, (300, 96, 33), torch.bfloat16, 9, 0.3)]
+    training_step(*states[1])
+    torch.cuda.synchronize()
+    want = [first, {k: v.clone() for k, v in states[1][3].items()}]
+    graphs = []
+    for st in states:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            training_step(*st)
+        graphs.append(g)
+    for st in states:
+        for v in st[3].values():
+            v.zero_()
+    torch.cuda.synchronize()
+    other = torch.cuda.Stream()
+    for _ in range(3):
+        graphs[0].replay()
+        with torch.cuda.stream(other):
+            graphs[1].replay()
+        torch.cuda.synchronize()
+    for st, w in zip(states, want):
+        assert all(torch.equal(w[k], st[3][k]) for k in w)
