@@ -49,11 +49,6 @@ __device__ __forceinline__ void load4(uint32_t type, const void* p, size_t at, b
   else if (type == kBf16) load4(reinterpret_cast<const __nv_bfloat16*>(p) + at, vec, n, v);
   else load4(reinterpret_cast<const __half*>(p) + at, vec, n, v);
 }
-__device__ __forceinline__ void store4(uint32_t type, void* p, size_t at, bool vec, int n, const float (&v)[4]) {
-  if (type == kF32) store4(reinterpret_cast<float*>(p) + at, vec, n, v);
-  else if (type == kBf16) store4(reinterpret_cast<__nv_bfloat16*>(p) + at, vec, n, v);
-  else store4(reinterpret_cast<__half*>(p) + at, vec, n, v);
-}
 
 __device__ __forceinline__ float sigmoid(float z) { return 1.f / (1.f + expf(-z)); }
 // relu'(0) = 0; gelu is z Phi(z) by the error function; silu is z sigmoid(z)
@@ -82,16 +77,26 @@ __device__ __forceinline__ void drop4(const Drop& d, uint64_t bits, float (&v)[4
   for (int i = 0; i < 4; ++i) v[i] = ((uint32_t)(bits >> (16 * i)) & 0xFFFFu) >= d.q ? v[i] * d.scale : 0.f;
 }
 
-// Four sums of row `row`, columns col .. col + 3 (col a multiple of 4) of a product with `cols` columns.
-__device__ __forceinline__ void finish4(const Epilogue& e, size_t row, uint32_t col, uint32_t cols, float (&v)[4]) {
-  const int n = (int)min(4u, cols - col);
-  if (e.bias) {
-    float b[4];
-    load4(e.bias_type, e.bias, col, false, n, b);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] += b[i];
+// x as three bf16 values whose sum is x to 24 bits: the upper 8 bits cut off, so that they cannot overflow, the rest to nearest.
+// An x that is infinite or no number is all in the first.
+__device__ __forceinline__ void three_parts(float x, uint16_t& h, uint16_t& m, uint16_t& l) {
+  const uint32_t u = __float_as_uint(x);
+  if ((u & 0x7F800000u) == 0x7F800000u) {
+    h = (uint16_t)((u & 0x007FFFFFu) ? 0x7FFFu : u >> 16);
+    m = l = 0;
+    return;
   }
-  if (e.pre) store4(e.out_type, e.pre, row * e.ld_pre + col, e.vec, n, v);
+  h = (uint16_t)(u >> 16);
+  const float r = x - __uint_as_float(u & 0xFFFF0000u);
+  const __nv_bfloat16 rm = __float2bfloat16_rn(r);
+  m = __bfloat16_as_ushort(rm);
+  l = __bfloat16_as_ushort(__float2bfloat16_rn(r - __bfloat162float(rm)));
+}
+
+// Four pre-activations (the bias is in them) of row `row`, columns col .. col + n - 1 of an array with `cols` columns.
+template <class Out>
+__device__ __forceinline__ void finish4(const Epilogue& e, size_t row, uint32_t col, uint32_t cols, int n, float (&v)[4]) {
+  if (e.pre) store4(static_cast<Out*>(e.pre) + row * e.ld_pre + col, e.vec, n, v);
   if (e.act) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = activate(e.act, v[i]);
@@ -99,11 +104,11 @@ __device__ __forceinline__ void finish4(const Epilogue& e, size_t row, uint32_t 
   if (e.drop.q) drop4(e.drop, drop_bits(e.drop, row, cols, col), v);
   if (e.residual) {
     float r[4];
-    load4(e.out_type, e.residual, row * e.ld_res + col, e.vec, n, r);
+    load4(static_cast<const Out*>(e.residual) + row * e.ld_res + col, e.vec, n, r);
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] += r[i];
   }
-  store4(e.out_type, e.out, row * e.ld_out + col, e.vec, n, v);
+  store4(static_cast<Out*>(e.out) + row * e.ld_out + col, e.vec, n, v);
 }
 
 }  // namespace layer

@@ -17,7 +17,19 @@ namespace {
 
 constexpr int kTile = 64, kStep = 16, kThreads = 256, kLd = kTile + 4;
 
-template <class T>
+template <class Out>
+__device__ __forceinline__ void with_bias(const Product& p, uint32_t row, uint32_t col, float (&v)[4]) {
+  const int n = (int)min(4u, p.n - col);
+  if (p.e.bias) {
+    float b[4];
+    load4(p.e.bias_type, p.e.bias, col, false, n, b);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] += b[i];
+  }
+  finish4<Out>(p.e, row, col, p.n, n, v);
+}
+
+template <class T, class Out>
 __global__ void __launch_bounds__(kThreads) product_fma_kernel(const Product p, const uint32_t tiles_n) {
   __shared__ __align__(16) float as[2][kStep][kLd], bs[2][kStep][kLd];
   __shared__ __align__(16) float sum[kTile][kLd];
@@ -73,7 +85,7 @@ __global__ void __launch_bounds__(kThreads) product_fma_kernel(const Product p, 
   if (split == 1) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (m0 + tr + i < p.m && n0 + tc < p.n) finish4(p.e, m0 + tr + i, n0 + tc, p.n, acc[i]);
+      if (m0 + tr + i < p.m && n0 + tc < p.n) with_bias<Out>(p, m0 + tr + i, n0 + tc, acc[i]);
     return;
   }
 #pragma unroll
@@ -89,7 +101,7 @@ __global__ void __launch_bounds__(kThreads) product_fma_kernel(const Product p, 
       const float4 s = *reinterpret_cast<const float4*>(cluster.map_shared_rank(&sum[r][c], q));
       v[0] += s.x; v[1] += s.y; v[2] += s.z; v[3] += s.w;
     }
-    finish4(p.e, m0 + r, n0 + c, p.n, v);
+    with_bias<Out>(p, m0 + r, n0 + c, v);
   }
   cluster.sync();   // a CTA's sums stay until the others have read them
 }
@@ -111,9 +123,11 @@ cudaError_t launch_product_fma(const Product& p, cudaStream_t s) {
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  if (p.type == kF32) return cudaLaunchKernelEx(&cfg, product_fma_kernel<float>, p, (uint32_t)tiles_n);
-  if (p.type == kBf16) return cudaLaunchKernelEx(&cfg, product_fma_kernel<__nv_bfloat16>, p, (uint32_t)tiles_n);
-  return cudaLaunchKernelEx(&cfg, product_fma_kernel<__half>, p, (uint32_t)tiles_n);
+  const uint32_t tn = (uint32_t)tiles_n;
+  if (p.type == kF32) return cudaLaunchKernelEx(&cfg, product_fma_kernel<float, float>, p, tn);
+  if (p.type == kBf16 && p.e.out_type == kF32) return cudaLaunchKernelEx(&cfg, product_fma_kernel<__nv_bfloat16, float>, p, tn);
+  if (p.type == kBf16) return cudaLaunchKernelEx(&cfg, product_fma_kernel<__nv_bfloat16, __nv_bfloat16>, p, tn);
+  return cudaLaunchKernelEx(&cfg, product_fma_kernel<__half, __half>, p, tn);
 }
 
 }  // namespace layer

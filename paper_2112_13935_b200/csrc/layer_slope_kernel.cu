@@ -39,7 +39,16 @@ __global__ void __launch_bounds__(kLanes* kRowLanes) slope_kernel(const SlopeLau
           v[i] = p.act == kRelu ? (f != 0.f ? v[i] : 0.f) : v[i] * f;
         }
       }
-      if (p.dz) store4(static_cast<T*>(p.dz) + r * p.ld_dz + col, vec, n, v);
+      if (p.dz && p.plane) {
+        Pack<uint16_t, 4> q[3] = {};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) three_parts(v[i], q[0].v[i], q[1].v[i], q[2].v[i]);   // (0 past the last column)
+        uint16_t* d = static_cast<uint16_t*>(p.dz) + r * p.ld_dz + col;
+#pragma unroll
+        for (int i = 0; i < 3; ++i) *reinterpret_cast<Pack<uint16_t, 4>*>(d + i * p.plane) = q[i];
+      } else if (p.dz) {
+        store4(static_cast<T*>(p.dz) + r * p.ld_dz + col, vec, n, v);
+      }
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[i] += v[i];
     }

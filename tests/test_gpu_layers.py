@@ -73,6 +73,23 @@ def test_dense_forward_options(type, over):
     check_forward(70, 131, 94, type, **over)
 
 
+# products the tensor cores take: odd edges of tiles and of k, few rows, a long k in parts, enough tiles for pairs of CTAs
+LARGE = [(300, 785, 300), (129, 1000, 640), (1, 8192, 8200), (70, 20000, 200), (4001, 131, 130), (2305, 72, 2100), (257, 513, 1024), (2049, 2048, 2056)]
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,n_in,n_out", LARGE)
+def test_dense_forward_large(rows, n_in, n_out, type):
+    check_forward(rows, n_in, n_out, type, act="relu", pre=True)
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,n_in,n_out", [(300, 785, 300), (100, 9000, 130), (2305, 72, 2100)])
+@pytest.mark.parametrize("over", [dict(pad=1, residual=True, act="silu", pre=True), dict(pad=3, shift=1, rate=0.1, residual=True), dict(pad=8, bias=False, residual=True, in_place=True)])
+def test_dense_forward_large_options(rows, n_in, n_out, type, over):
+    check_forward(rows, n_in, n_out, type, **over)
+
+
 def check_backward(rows, n_in, n_out, type, act="none", rate=0.0, pad=0, shift=0, accumulate=False, want=("dx", "dw", "db"), seed=2):
     t = lh.TYPES[type]
     d = layer_inputs(rows, n_in, n_out, t, seed)
@@ -120,6 +137,19 @@ def test_dense_backward_sizes(rows, n_in, n_out, type):
     dict(want=("dw", "db"), rate=0.2)])
 def test_dense_backward_options(type, over):
     check_backward(90, 77, 139, type, **over)
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,n_in,n_out", LARGE)
+def test_dense_backward_large(rows, n_in, n_out, type):
+    check_backward(rows, n_in, n_out, type, act="relu")
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,n_in,n_out", [(300, 785, 300), (9000, 100, 130), (72, 2305, 2100)])
+@pytest.mark.parametrize("over", [dict(), dict(pad=1), dict(pad=8), dict(pad=3, shift=1, act="silu", rate=0.1), dict(accumulate=True, act="relu"), dict(want=("dw",), pad=8), dict(want=("dx", "db"))])
+def test_dense_backward_large_options(rows, n_in, n_out, type, over):
+    check_backward(rows, n_in, n_out, type, **over)
 
 
 def test_dense_backward_over_no_rows_is_zero():
