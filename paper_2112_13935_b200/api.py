@@ -256,39 +256,42 @@ def _dtype(t) -> int:
     if not _dtypes:
         import torch
         _dtypes.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
-    if t not in _dtypes:
-        raise AetError(1, f"element type {t} is not float32, bfloat16 or float16")
-    return _dtypes[t]
+    try:
+        return _dtypes[t]
+    except KeyError:
+        raise AetError(1, f"element type {t} is not float32, bfloat16 or float16") from None
 
 
-def _here(device) -> int:
-    """The current stream of the current device, which the tensors have to be on."""
+def _raw_stream(t, stream):
+    """The stream given, or the current one, of the current device, which the tensors have to be on."""
     import torch
-    if device.type != "cuda" or device.index != torch.cuda.current_device():
-        raise AetError(1, f"tensors have to be on the current CUDA device, not on {device}")
-    return torch.cuda.current_stream().cuda_stream
-
-
-def _raw_stream(t, stream) -> int:
-    here = _here(t.device)
-    return here if stream is None else stream if isinstance(stream, int) else stream.cuda_stream
+    dev = torch._C._cuda_getDevice() if t.is_cuda else -2     # (torch.cuda.current_device and current_stream take longer than the call)
+    if t.get_device() != dev:
+        raise AetError(1, f"tensors have to be on the current CUDA device, not on {t.device}")
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(dev)
+    return stream if isinstance(stream, int) else stream.cuda_stream
 
 
 def _at(t, like, shape, what, ld=None):
-    """Address of a matrix or vector of `like`'s type and device (None: null)."""
+    """Address of a matrix (its rows `ld` elements apart) or vector of `like`'s type and device (None: null)."""
     if t is None:
         return None
-    if t.dtype is not like.dtype or t.device != like.device or t.shape != shape:
+    if t.dtype is not like.dtype or t.shape != shape or t.get_device() != like.get_device():
         raise AetError(1, f"{what}: {tuple(t.shape)} of {t.dtype} on {t.device}, expected {tuple(shape)} of {like.dtype} on {like.device}")
-    strides = t.stride()
-    if t.numel() and ((shape[-1] > 1 and strides[-1] != 1) or (ld is not None and shape[0] > 1 and strides[0] != ld)):
-        raise AetError(1, f"{what}: strides {strides}, expected rows {ld} elements apart of neighbouring elements")
+    s = t.stride()
+    if s != ((1,) if ld is None and len(s) == 1 else (ld, 1)) and t.numel():     # (what an index of one value strides by does not matter)
+        if (shape[-1] > 1 and s[-1] != 1) or (ld is not None and shape[0] > 1 and s[0] != ld):
+            raise AetError(1, f"{what}: strides {s}, expected rows {ld} elements apart of neighbouring elements")
     return t.data_ptr()
 
 
-def _ld(t) -> int:
-    """Elements between the rows of a matrix."""
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+def _row_major(t, like, shape, what):
+    """Address and ld of a matrix whose rows may be any distance apart."""
+    if t is None:
+        return None, 0
+    ld = t.stride(0) if len(shape) == 2 and shape[0] > 1 else shape[-1]
+    return _at(t, like, shape, what, ld), ld
 
 
 def aet_dropout_spec(seed: int, client: int = 0, counter: int = 0, rate: float = 0.0):
@@ -301,8 +304,8 @@ def aet_dropout(drop, x, y, residual=None, stream=None):
     if len(shape) != 2:
         raise AetError(1, "x: a matrix is expected")
     _check(None, _lib.load().aet_dropout(
-        _dtype(x.dtype), shape[0], shape[1], C.addressof(drop), _at(x, x, shape, "x"), _ld(x),
-        _at(residual, x, shape, "residual"), 0 if residual is None else _ld(residual), _at(y, x, shape, "y"), _ld(y), _raw_stream(x, stream)))
+        _dtype(x.dtype), shape[0], shape[1], C.addressof(drop), *_row_major(x, x, shape, "x"), *_row_major(residual, x, shape, "residual"),
+        *_row_major(y, x, shape, "y"), _raw_stream(x, stream)))
 
 
 def aet_cross_entropy(logits, labels, loss=None, dlogits=None, top=None, weight=None, scale: float = 1.0, stream=None):
@@ -311,13 +314,14 @@ def aet_cross_entropy(logits, labels, loss=None, dlogits=None, top=None, weight=
     shape = logits.shape
     if len(shape) != 2:
         raise AetError(1, "logits: a matrix is expected")
-    for t, kind, what in ((labels, torch.int32, "labels"), (loss, torch.float32, "loss"), (top, torch.int32, "top"), (weight, torch.float32, "weight")):
-        if t is not None and (t.dtype is not kind or t.shape != shape[:1] or not t.is_contiguous() or t.device != logits.device):
+    at = []
+    for t, kind, what in ((labels, torch.int32, "labels"), (weight, torch.float32, "weight"), (loss, torch.float32, "loss"), (top, torch.int32, "top")):
+        if t is not None and (t.dtype is not kind or t.shape != shape[:1] or not t.is_contiguous() or t.get_device() != logits.get_device()):
             raise AetError(1, f"{what}: {tuple(t.shape)} of {t.dtype} on {t.device}, expected {shape[0]} neighbouring {kind} on {logits.device}")
-    p = lambda t: None if t is None else t.data_ptr()   # noqa: E731
+        at.append(None if t is None else t.data_ptr())
     _check(None, _lib.load().aet_cross_entropy(
-        _dtype(logits.dtype), shape[0], shape[1], _at(logits, logits, shape, "logits"), _ld(logits), p(labels), p(weight), scale, p(loss),
-        _at(dlogits, logits, shape, "dlogits"), 0 if dlogits is None else _ld(dlogits), p(top), _raw_stream(logits, stream)))
+        _dtype(logits.dtype), shape[0], shape[1], *_row_major(logits, logits, shape, "logits"), at[0], at[1], scale, at[2],
+        *_row_major(dlogits, logits, shape, "dlogits"), at[3], _raw_stream(logits, stream)))
 
 
 def aet_dense(n_in: int, n_out: int, dtype=None, act: str = "none", dropout=None, ld_in: int = 0, ld_out: int = 0, ld_w: int = 0, flags: int = 0, **lds):
@@ -351,7 +355,7 @@ def aet_dense_workspace(d, rows: int, backward: bool = False) -> int:
 def _space(workspace, like):
     if workspace is None:
         return None, 0
-    if workspace.device != like.device or not workspace.is_contiguous():
+    if workspace.get_device() != like.get_device() or not workspace.is_contiguous():
         raise AetError(1, "workspace: a contiguous tensor on the layer's device is expected")
     return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 

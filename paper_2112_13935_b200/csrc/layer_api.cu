@@ -172,7 +172,7 @@ extern "C" aet_status aet_cross_entropy(uint32_t dtype, size_t rows, uint32_t cl
                                         const float* weight, float scale, float* loss, void* dlogits, size_t ld_dlogits, int32_t* top,
                                         void* cuda_stream) {
   if (dtype > AET_F16) return arg("unknown dtype");
-  if (!classes || classes > kMostRows || rows > kMostRows) return arg("classes are 1 to 2^31 - 1, rows up to 2^31 - 1");
+  if (!classes || classes > 1u << 30 || rows > kMostRows) return arg("classes are 1 to 2^30, rows up to 2^31 - 1");
   if (!rows) return AET_OK;
   if (!logits || !labels) return arg("null argument");
   if (!ld) ld = classes;

@@ -54,7 +54,7 @@ def loss(**over):
 
 
 @pytest.mark.parametrize("over,text", [
-    (dict(dtype=9), "dtype"), (dict(classes=0), "classes"), (dict(classes=1 << 31), "classes"), (dict(rows=1 << 31), "rows"), (dict(logits=None), "null"),
+    (dict(dtype=9), "dtype"), (dict(classes=0), "classes"), (dict(classes=(1 << 30) + 1), "classes"), (dict(rows=1 << 31), "rows"), (dict(logits=None), "null"),
     (dict(labels=None), "null"), (dict(ld=2), "ld"), (dict(ld_d=1), "ld"), (dict(logits=P + 2), "element size"), (dict(labels=P + 2), "element size"),
     (dict(weight=P + 1), "element size"), (dict(loss=P + 2), "element size"), (dict(top=P + 2), "element size"), (dict(dlogits=P + 1, dtype=1), "element size")])
 def test_loss_refusals(over, text):
