@@ -240,6 +240,31 @@ aet_status aet_get_node_model(aet_handle* h, uint32_t node, float* out, size_t n
 aet_status aet_get_event_log(aet_handle* h, aet_event* out, size_t capacity,
                              size_t* n_events, aet_summary* summary);
 
+/* Logits of `n` rows x [n, dims[0]] by the model of node `node` (as
+ * aet_get_node_model has it): [n, classes] fp32, host or device pointers.  Softmax
+ * regression and ReLU MLPs; precision 1 rounds inputs, weights and hidden
+ * activations to bf16 as its rounds do.  Runs on the layer operators below, in
+ * chunks of rows whose workspace the handle keeps.  Synchronises `cuda_stream`.
+ * Errors: AET_ERR_ARG, AET_ERR_CONFIG (model 2), AET_ERR_NOMEM, AET_ERR_CUDA, and
+ * what aet_get_node_model reports. */
+aet_status aet_predict(aet_handle* h, uint32_t node, const float* x, uint32_t n, float* logits,
+                       void* cuda_stream);
+
+/* Loss (Eq. 1: the mean of f(w; xi) over these rows, with the l2 term), how many of
+ * the rows the model gets right (Section 5's accuracy; ties go to the lower class),
+ * and the loss's gradient (n_params floats, host or device pointer) of node `node`'s
+ * model on rows x [n, dims[0]] with classes y [n] (host or device pointers).  loss,
+ * correct and gradient may be null.  drop (null: none): dropout behind each hidden
+ * layer's activation, the masks of hidden layer l drawn behind those of the layers in
+ * front of it, n * ceil(width / 4) draws each; loss and gradient are then those of
+ * the thinned model.  Nothing of the handle's run changes.  Synchronises
+ * `cuda_stream`.  Errors as aet_predict, AET_ERR_ARG (a label out of range),
+ * AET_ERR_NUMERIC (the loss is not finite); outputs are then untouched. */
+struct aet_dropout_spec_s;
+aet_status aet_evaluate(aet_handle* h, uint32_t node, const float* x, const int32_t* y, uint32_t n,
+                        const struct aet_dropout_spec_s* drop, double* loss, uint64_t* correct,
+                        float* gradient, void* cuda_stream);
+
 /* Update sum number `seq` of the most recent aet_run_rounds (host or device
  * pointer, n_params floats).  Needs AET_FLAG_KEEP_UPDATE_SUMS (AET_ERR_STATE
  * without it: rows are recycled in both topologies).  In the ring topology
@@ -349,7 +374,7 @@ typedef enum {
  * q = round(65536 rate), and multiplied by 65536 / (65536 - q) otherwise.  A call
  * on R rows uses up R * ceil(C / 4) draws: advance `counter` by that for other
  * masks.  rate 0: nothing is dropped. */
-typedef struct {
+typedef struct aet_dropout_spec_s {
   uint64_t seed, counter;
   uint32_t client;
   float rate; /* 0 <= rate, q < 65536 */

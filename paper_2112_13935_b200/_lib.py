@@ -87,6 +87,9 @@ PROTOTYPES = {
     "aet_last_error": (C.c_char_p, [C.c_void_p]),
     "aet_round_no_alloc": (C.c_int, [C.POINTER(AetConfig), C.c_uint32, C.c_uint32, C.c_void_p, C.c_void_p,
                                      C.c_uint32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "aet_predict": (C.c_int, [C.c_void_p, C.c_uint32, C.c_void_p, C.c_uint32, C.c_void_p, C.c_void_p]),
+    "aet_evaluate": (C.c_int, [C.c_void_p, C.c_uint32, C.c_void_p, C.c_void_p, C.c_uint32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                               C.c_void_p]),
     "aet_dropout": (C.c_int, [C.c_uint32, C.c_size_t, C.c_uint32, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p, C.c_size_t,
                               C.c_void_p, C.c_size_t, C.c_void_p]),
     "aet_cross_entropy": (C.c_int, [C.c_uint32, C.c_size_t, C.c_uint32, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p, C.c_float,

@@ -137,6 +137,22 @@ def aet_get_update_sum(h, seq: int, out=None, stream=None):
     return out
 
 
+def aet_predict(h, node: int, x, logits=None, classes=None, stream=None):
+    """Logits [n, classes] of a node's model for the rows of x; host or device arrays (logits default: a numpy array)."""
+    if logits is None:
+        logits = np.empty((x.shape[0], classes), dtype=np.float32)
+    _check(h, _lib.load().aet_predict(h, node, _ptr(x), x.shape[0], _ptr(logits), _stream(stream)))
+    return logits
+
+
+def aet_evaluate(h, node: int, x, y, dropout=None, gradient=None, stream=None):
+    """(loss, rows the model gets right) of a node's model on rows x with classes y; gradient: where the loss's gradient goes."""
+    loss, right = C.c_double(), C.c_uint64()
+    _check(h, _lib.load().aet_evaluate(h, node, _ptr(x), _ptr(y), x.shape[0], None if dropout is None else C.addressof(dropout),
+                                       C.addressof(loss), C.addressof(right), _ptr(gradient), _stream(stream)))
+    return float(loss.value), int(right.value)
+
+
 def _events_from(arr, n):
     names = [f for f, _ in AetEvent._fields_]
     return [{f: int(getattr(arr[k], f)) for f in names} for k in range(n)]
@@ -412,6 +428,12 @@ class Session:
 
     def model(self):
         return aet_get_global_model(self.h, stream=self.stream)
+
+    def predict(self, x, node=0):
+        return aet_predict(self.h, node, x, classes=self.cfg["dims"][-1], stream=self.stream)
+
+    def evaluate(self, x, y, node=0, dropout=None, gradient=None):
+        return aet_evaluate(self.h, node, x, y, dropout, gradient, self.stream)
 
     def log(self, raw=False):
         return aet_get_event_log(self.h, raw)

@@ -16,6 +16,7 @@
 #include "aet_kernels.h"
 #include "aet_rng.h"
 #include "aet_schedule.h"
+#include "evaluate.h"
 
 using namespace aet;
 
@@ -251,6 +252,7 @@ struct aet_handle {
   DevBuf<uint64_t> d_keys;
   DevBuf<uint32_t> d_H;
   DevBuf<float> w, w0, snaps, U, work, act, dbg;
+  DevBuf<char> eval;              // workspace of aet_predict and aet_evaluate
   DevBuf<float> node_w;           // topology 1: [n_clients, stride], every node's own model
   DevBuf<RingApplyDesc> d_ring_applies;
   DevBuf<RingOp> d_ring_ops;
@@ -589,7 +591,7 @@ aet_status aet_destroy(aet_handle* h) {
   h->arena.release();
   h->d_clients.release(); h->d_keys.release(); h->d_H.release();
   h->w.release(); h->w0.release(); h->snaps.release(); h->U.release();
-  h->work.release(); h->act.release(); h->dbg.release();
+  h->work.release(); h->act.release(); h->dbg.release(); h->eval.release();
   h->node_w.release(); h->d_ring_applies.release(); h->d_ring_ops.release();
   h->d_tasks.release(); h->d_plan.release();
   h->d_trig.release(); h->d_alog.release();
@@ -894,6 +896,102 @@ aet_status aet_get_node_model(aet_handle* h, uint32_t node, float* out, size_t n
   if (node >= h->cfg.n_clients) return fail(h, AET_ERR_ARG, "node index out of range");
   // client-server: at quiescence every client slot equals the server model
   return read_model(h, h->cfg.topology == 1 ? h->node_w.p + (size_t)node * h->stride : h->w_cur(), out, (cudaStream_t)cuda_stream);
+}
+
+}  // extern "C"
+
+namespace {
+
+bool on_device(const void* p) {
+  cudaPointerAttributes a{};
+  const bool yes = cudaPointerGetAttributes(&a, p) == cudaSuccess && (a.type == cudaMemoryTypeDevice || a.type == cudaMemoryTypeManaged);
+  cudaGetLastError();
+  return yes;
+}
+
+// Rows through node `node`'s model, chunk by chunk: logits out (a predict), or loss, right answers and gradient (y not null).
+aet_status run_evaluation(aet_handle* h, uint32_t node, const float* x, const int32_t* y, uint32_t n, const aet_dropout_spec* drop, float* logits,
+                          double* loss, uint64_t* correct, float* gradient, cudaStream_t s) {
+  if (h->cfg.model == 2) return fail(h, AET_ERR_CONFIG, "the convolutional classifier has no evaluation: softmax regression and ReLU MLPs only");
+  if (node >= h->cfg.n_clients) return fail(h, AET_ERR_ARG, "node index out of range");
+  if (!n) return fail(h, AET_ERR_ARG, "no rows");
+  EvalModel m{};
+  m.n_layers = h->cfg.n_layers;
+  for (int i = 0; i < 8; ++i) m.dims[i] = h->cfg.dims[i];
+  m.bf16 = h->cfg.precision == 1;
+  m.l2 = h->cfg.l2;
+  if (drop) {
+    layer::Drop d;
+    if (const char* why = layer::read_drop(*drop, d)) return fail(h, AET_ERR_ARG, why);
+    m.drop = *drop;
+  }
+  const float* w = h->cfg.topology == 1 ? h->node_w.p + (size_t)node * h->stride : h->w_cur();
+  const size_t D = m.dims[0], classes = m.dims[m.n_layers], chunk = eval_chunk(m, n), last = n % chunk ? n % chunk : chunk;
+  // workspace: the tally, a gradient, rows, labels and logits that come from or go to the host, the layers'
+  const bool x_here = on_device(x), y_here = !y || on_device(y), z_here = !logits || on_device(logits);
+  if ((x_here && (uintptr_t)x % 4) || (y && y_here && (uintptr_t)y % 4) || (logits && z_here && (uintptr_t)logits % 4))
+    return fail(h, AET_ERR_ARG, "a device pointer is not a multiple of four");
+  size_t at = 0;
+  const auto take = [&](size_t bytes) { const size_t p = at; at += (bytes + 255) / 256 * 256; return p; };
+  const size_t o_tally = take(sizeof(Tally)), o_grad = take(gradient ? (size_t)h->P * 4 : 0), o_x = take(x_here ? 0 : chunk * D * 4),
+               o_y = take(y_here ? 0 : chunk * 4), o_z = take(z_here ? 0 : chunk * classes * 4);
+  const size_t a = eval_space(m, chunk, y != nullptr, gradient != nullptr), b = eval_space(m, last, y != nullptr, gradient != nullptr);
+  const size_t o_layers = take(a > b ? a : b);
+  if (!h->eval.reserve(at)) return fail(h, AET_ERR_NOMEM, "device allocation failed");
+  char* ws = h->eval.p;
+  Tally* tally = reinterpret_cast<Tally*>(ws + o_tally);
+  float* g = gradient ? reinterpret_cast<float*>(ws + o_grad) : nullptr;
+  h->last_stream = s;
+  AET_CUDA(h, cudaMemsetAsync(tally, 0, sizeof(Tally), s));
+  for (size_t r = 0; r < n; r += chunk) {
+    const size_t rows = n - r < chunk ? n - r : chunk;
+    const float* xr = x + r * D;
+    const int32_t* yr = y ? y + r : nullptr;
+    float* zr = logits ? logits + r * classes : nullptr;
+    if (!x_here) {
+      AET_CUDA(h, cudaMemcpyAsync(ws + o_x, xr, rows * D * 4, cudaMemcpyDefault, s));
+      xr = reinterpret_cast<float*>(ws + o_x);
+    }
+    if (!y_here) {
+      AET_CUDA(h, cudaMemcpyAsync(ws + o_y, yr, rows * 4, cudaMemcpyDefault, s));
+      yr = reinterpret_cast<int32_t*>(ws + o_y);
+    }
+    AET_CUDA(h, eval_rows(m, w, xr, yr, r, rows, n, z_here ? zr : reinterpret_cast<float*>(ws + o_z), tally, g, ws + o_layers, s));
+    if (!z_here) AET_CUDA(h, cudaMemcpyAsync(zr, ws + o_z, rows * classes * 4, cudaMemcpyDefault, s));
+  }
+  if (y && m.l2 != 0.f) AET_CUDA(h, eval_l2(m, w, n, tally, g, s));
+  Tally t{};
+  AET_CUDA(h, cudaMemcpyAsync(&t, tally, sizeof(t), cudaMemcpyDefault, s));
+  AET_CUDA(h, cudaStreamSynchronize(s));
+  if (aet_status ds = check_device_status(h)) return ds;
+  if (!y) return AET_OK;
+  if (t.bad_labels) return fail(h, AET_ERR_ARG, "a label is out of range");
+  t.loss /= (double)n;
+  if (!isfinite(t.loss)) return fail(h, AET_ERR_NUMERIC, "the loss is not finite: a non-finite value in the model or in the rows");
+  if (gradient) {
+    AET_CUDA(h, cudaMemcpyAsync(gradient, g, (size_t)h->P * 4, cudaMemcpyDefault, s));
+    AET_CUDA(h, cudaStreamSynchronize(s));
+  }
+  if (loss) *loss = t.loss;
+  if (correct) *correct = t.correct;
+  return AET_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+aet_status aet_predict(aet_handle* h, uint32_t node, const float* x, uint32_t n, float* logits, void* cuda_stream) {
+  if (!h) return AET_ERR_ARG;
+  if (!x || !logits) return fail(h, AET_ERR_ARG, "null argument");
+  return run_evaluation(h, node, x, nullptr, n, nullptr, logits, nullptr, nullptr, nullptr, (cudaStream_t)cuda_stream);
+}
+
+aet_status aet_evaluate(aet_handle* h, uint32_t node, const float* x, const int32_t* y, uint32_t n, const aet_dropout_spec* drop, double* loss,
+                        uint64_t* correct, float* gradient, void* cuda_stream) {
+  if (!h) return AET_ERR_ARG;
+  if (!x || !y) return fail(h, AET_ERR_ARG, "null argument");
+  return run_evaluation(h, node, x, y, n, drop, nullptr, loss, correct, gradient, (cudaStream_t)cuda_stream);
 }
 
 aet_status aet_get_update_sum(aet_handle* h, uint32_t seq, float* out, size_t n_params, void* cuda_stream) {

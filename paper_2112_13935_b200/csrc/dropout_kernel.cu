@@ -1,47 +1,71 @@
 // Dropout whose mask is never stored: y = residual + drop(x), each element's sixteen random bits a function of where it stands.
 //
 // The counter-based generator costs some 22 integer instructions a draw of 64 bits; with four elements to a draw a bf16 array stays
-// bound by memory (about 5.8 elements a cycle and SM at the copy rate, 22 issue slots each).  The gradient is the same call on dy.
+// bound by memory (about 5.8 elements a cycle and SM at the copy rate, 22 issue slots each).  A thread keeps its 16 bytes of columns and
+// goes down the rows, three at a time with all their loads under way.  The gradient is the same call on dy.
 #include <cuda_runtime.h>
 
-#include "layer_common.cuh"
+#include "layer_rows.cuh"
 
 namespace aet {
 namespace layer {
 namespace {
 
-template <class T, bool kVec>
-__global__ void __launch_bounds__(256) dropout_kernel(size_t rows, uint32_t cols, Drop d, const T* x, size_t ld_x, const T* res, size_t ld_res,
-                                                      T* y, size_t ld_y, uint64_t groups) {
-  const uint32_t per = (cols + 3) / 4;
-  for (uint64_t g = (uint64_t)blockIdx.x * 256 + threadIdx.x; g < groups; g += (uint64_t)gridDim.x * 256) {
-    const uint64_t row = g / per;
-    const uint32_t col = (uint32_t)(g - row * per) * 4;
-    const int n = (int)min(4u, cols - col);
-    float v[4];
-    load4(x + row * ld_x + col, kVec, n, v);
-    if (d.q) drop4(d, draw(d.key, d.counter + g), v);
-    if (res) {
-      float r[4];
-      load4(res + row * ld_res + col, kVec, n, r);
+constexpr int kThreads = 256, kRows = 3;
+
+template <class T, int N, bool kVec>
+__global__ void __launch_bounds__(kThreads, 3) dropout_kernel(const size_t rows, const uint32_t cols, const Drop d, const T* x, const size_t ld_x, const T* res,
+                                                           const size_t ld_res, T* y, const size_t ld_y, const uint32_t log) {
+  const uint32_t col = ((blockIdx.x << log) + (threadIdx.x & ((1u << log) - 1))) * N;
+  if (col >= cols) return;
+  const int n = (int)min((uint32_t)N, cols - col);
+  const bool whole = kVec && n == N;
+  const size_t step = (size_t)gridDim.y * (kThreads >> log);     // rows between two of a thread's
+  for (size_t r0 = (size_t)blockIdx.y * (kThreads >> log) + (threadIdx.x >> log); r0 < rows; r0 += kRows * step) {
+    Words<T, N> q[kRows], e[kRows];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] += r[i];
+    for (int i = 0; i < kRows; ++i) {
+      const size_t r = r0 + i * step;
+      if (r >= rows) break;
+      q[i] = load_words<T, N>(x + r * ld_x + col, whole, n);
+      if (res) e[i] = load_words<T, N>(res + r * ld_res + col, whole, n);
     }
-    store4(y + row * ld_y + col, kVec, n, v);
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+      const size_t r = r0 + i * step;
+      if (r >= rows) break;
+      keep_words(q[i]);
+      float v[N];
+      unpack<T, N>(q[i], v);
+      if (d.q) drop_n<N>(d, drop_at(d, r, cols, col), v);
+      if (res) {
+        keep_words(e[i]);
+        float a[N];
+        unpack<T, N>(e[i], a);
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] += a[k];
+      }
+      store_n<T, N>(y + r * ld_y + col, whole, n, v);
+    }
   }
 }
 
+template <class T, int N, bool kVec>
+cudaError_t go(size_t rows, uint32_t cols, const Drop& d, const void* x, size_t ld_x, const void* res, size_t ld_res, void* y, size_t ld_y, cudaStream_t s) {
+  const uint32_t log = log_lanes<N>(cols);
+  const uint64_t across = (((uint64_t)cols + N - 1) / N + (1u << log) - 1) >> log;     // CTAs across the columns
+  // eight CTAs for each of 148 SMs, which go round the rows
+  const uint64_t at_once = (uint64_t)(kThreads >> log) * kRows, most = (rows + at_once - 1) / at_once, want = (148 * 8 + across - 1) / across;
+  dropout_kernel<T, N, kVec><<<dim3((unsigned)across, (unsigned)(most < want ? most : want)), kThreads, 0, s>>>(
+      rows, cols, d, (const T*)x, ld_x, (const T*)res, ld_res, (T*)y, ld_y, log);
+  return cudaGetLastError();
+}
 template <class T>
 cudaError_t run(size_t rows, uint32_t cols, const Drop& d, const void* x, size_t ld_x, const void* res, size_t ld_res, void* y, size_t ld_y,
                 cudaStream_t s) {
-  const uint64_t groups = (uint64_t)rows * ((cols + 3) / 4);
-  const uint64_t want = (groups + 255) / 256;
-  const unsigned grid = (unsigned)(want < 148 * 64 ? want : 148 * 64);
-  const size_t q = 4 * sizeof(T);
-  const bool vec = (((uintptr_t)x | (uintptr_t)y | (uintptr_t)res) % q) == 0 && ((ld_x | ld_y | (res ? ld_res : 0)) % 4) == 0;
-  if (vec) dropout_kernel<T, true><<<grid, 256, 0, s>>>(rows, cols, d, (const T*)x, ld_x, (const T*)res, ld_res, (T*)y, ld_y, groups);
-  else dropout_kernel<T, false><<<grid, 256, 0, s>>>(rows, cols, d, (const T*)x, ld_x, (const T*)res, ld_res, (T*)y, ld_y, groups);
-  return cudaGetLastError();
+  constexpr int N = 16 / (int)sizeof(T);
+  const bool vec = (((uintptr_t)x | (uintptr_t)y | (uintptr_t)res) % 16) == 0 && ((ld_x | ld_y | (res ? ld_res : 0)) % N) == 0;
+  return vec ? go<T, N, true>(rows, cols, d, x, ld_x, res, ld_res, y, ld_y, s) : go<T, 4, false>(rows, cols, d, x, ld_x, res, ld_res, y, ld_y, s);
 }
 
 }  // namespace

@@ -3,6 +3,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "aet_rng.h"
 #include "layer_ops.h"
 
@@ -17,64 +19,140 @@ template <> __device__ __forceinline__ float from_f32<float>(float v) { return v
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
 
-// N neighbouring elements as one access (N elements from an address that is a multiple of their size)
-template <class T, int N> struct alignas(sizeof(T) * N) Pack { T v[N]; };
-
-template <class T>
-__device__ __forceinline__ void load4(const T* p, bool vec, int n, float (&v)[4]) {   // n: how many of the four there are
-  if (vec && n == 4) {
-    const Pack<T, 4> q = *reinterpret_cast<const Pack<T, 4>*>(p);
+// N neighbouring elements as one access of words (from an address that is a multiple of their size).  The words are taken apart and put
+// together by hand: structs of 16-bit elements are copied one by one, and arrays of them go to local memory.
+template <int kWords> struct WordsOf;
+template <> struct WordsOf<2> { using type = uint2; };
+template <> struct WordsOf<4> { using type = uint4; };
+template <class T, int N> using Words = typename WordsOf<N * (int)sizeof(T) / 4>::type;
+__device__ __forceinline__ void split_words(const uint2& q, uint32_t (&w)[2]) { w[0] = q.x; w[1] = q.y; }
+__device__ __forceinline__ void split_words(const uint4& q, uint32_t (&w)[4]) { w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w; }
+__device__ __forceinline__ uint2 join_words(const uint32_t (&w)[2]) { return make_uint2(w[0], w[1]); }
+__device__ __forceinline__ uint4 join_words(const uint32_t (&w)[4]) { return make_uint4(w[0], w[1], w[2], w[3]); }
+template <class T, int N>
+__device__ __forceinline__ void unpack(const Words<T, N>& q, float (&v)[N]) {
+  uint32_t w[N * sizeof(T) / 4];
+  split_words(q, w);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = to_f32(q.v[i]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = i < n ? to_f32(p[i]) : 0.f;
+  for (int i = 0; i < N * (int)sizeof(T) / 4; ++i) {
+    if constexpr (sizeof(T) == 4) {
+      v[i] = __uint_as_float(w[i]);
+    } else if constexpr (std::is_same<T, __half>::value) {
+      v[2 * i] = __half2float(__ushort_as_half((unsigned short)w[i]));
+      v[2 * i + 1] = __half2float(__ushort_as_half((unsigned short)(w[i] >> 16)));
+    } else {
+      v[2 * i] = __uint_as_float(w[i] << 16);
+      v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
   }
 }
-template <class T>
-__device__ __forceinline__ void store4(T* p, bool vec, int n, const float (&v)[4]) {
-  if (vec && n == 4) {
-    Pack<T, 4> q;
+template <class T, int N>
+__device__ __forceinline__ Words<T, N> pack(const float (&v)[N]) {
+  uint32_t w[N * sizeof(T) / 4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) q.v[i] = from_f32<T>(v[i]);
-    *reinterpret_cast<Pack<T, 4>*>(p) = q;
+  for (int i = 0; i < N * (int)sizeof(T) / 4; ++i) {
+    if constexpr (sizeof(T) == 4) {
+      w[i] = __float_as_uint(v[i]);
+    } else if constexpr (std::is_same<T, __half>::value) {
+      const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+      w[i] = (uint32_t)__half_as_ushort(__low2half(h)) | (uint32_t)__half_as_ushort(__high2half(h)) << 16;
+    } else {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+      w[i] = (uint32_t)__bfloat16_as_ushort(__low2bfloat16(h)) | (uint32_t)__bfloat16_as_ushort(__high2bfloat16(h)) << 16;
+    }
+  }
+  return join_words(w);
+}
+// The words of N neighbouring elements, as they are (kept so until they are used, rows that are under way cost half the registers).
+template <class T, int N>
+__device__ __forceinline__ Words<T, N> load_words(const T* p, bool whole, int n) {
+  if (whole) return *reinterpret_cast<const Words<T, N>*>(p);
+  float v[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = i < n ? to_f32(p[i]) : 0.f;
+  return pack<T, N>(v);
+}
+__device__ __forceinline__ void keep_words(uint2& q) { asm volatile("" : "+r"(q.x), "+r"(q.y)); }
+__device__ __forceinline__ void keep_words(uint4& q) { asm volatile("" : "+r"(q.x), "+r"(q.y), "+r"(q.z), "+r"(q.w)); }
+// N neighbouring elements in registers; `whole`: all N are there and may be touched at once (n: how many there are otherwise).
+template <class T, int N>
+__device__ __forceinline__ void load_n(const T* p, bool whole, int n, float (&v)[N]) {
+  if (whole) {
+    unpack<T, N>(*reinterpret_cast<const Words<T, N>*>(p), v);
   } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < N; ++i) v[i] = i < n ? to_f32(p[i]) : 0.f;
+  }
+}
+template <class T, int N>
+__device__ __forceinline__ void store_n(T* p, bool whole, int n, const float (&v)[N]) {
+  if (whole) {
+    *reinterpret_cast<Words<T, N>*>(p) = pack<T, N>(v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
       if (i < n) p[i] = from_f32<T>(v[i]);
   }
 }
-__device__ __forceinline__ void load4(uint32_t type, const void* p, size_t at, bool vec, int n, float (&v)[4]) {
-  if (type == kF32) load4(reinterpret_cast<const float*>(p) + at, vec, n, v);
-  else if (type == kBf16) load4(reinterpret_cast<const __nv_bfloat16*>(p) + at, vec, n, v);
-  else load4(reinterpret_cast<const __half*>(p) + at, vec, n, v);
+__device__ __forceinline__ void load4(uint32_t type, const void* p, size_t at, bool whole, int n, float (&v)[4]) {
+  if (type == kF32) load_n<float, 4>(reinterpret_cast<const float*>(p) + at, whole, n, v);
+  else if (type == kBf16) load_n<__nv_bfloat16, 4>(reinterpret_cast<const __nv_bfloat16*>(p) + at, whole, n, v);
+  else load_n<__half, 4>(reinterpret_cast<const __half*>(p) + at, whole, n, v);
 }
 
-__device__ __forceinline__ float sigmoid(float z) { return 1.f / (1.f + expf(-z)); }
-// relu'(0) = 0; gelu is z Phi(z) by the error function; silu is z sigmoid(z)
-__device__ __forceinline__ float activate(uint32_t act, float z) {
+// Activations for values that are stored as T.  relu'(0) = 0; gelu is z Phi(z) by the error function; silu is z sigmoid(z).
+// 16-bit results take a shorter way: exponentials by ex2.approx, and Phi(z) = 1 - P(t) e^(-z^2/2) / 2 for z >= 0 with t = 1 / (1 + p |z| / sqrt 2)
+// and Hastings' polynomial P (Abramowitz and Stegun 7.1.26), which is within 1.5e-7 / 2 of Phi everywhere and shares its exponential with
+// the density that the slope needs.
+template <class T> __device__ __forceinline__ float sigmoid(float z) {
+  return sizeof(T) == 4 ? __fdividef(1.f, 1.f + expf(-z)) : __fdividef(1.f, 1.f + __expf(-z));
+}
+__device__ __forceinline__ float hastings(float z, float& gauss) {   // Phi(z), and e^(-z^2/2)
+  const float x = fabsf(z) * 0.70710678118654752f, t = __fdividef(1.f, fmaf(0.3275911f, x, 1.f));
+  gauss = __expf(-0.5f * z * z);
+  const float p = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+  const float tail = 0.5f * p * gauss;
+  return z >= 0.f ? 1.f - tail : tail;
+}
+template <class T> __device__ __forceinline__ float activate(uint32_t act, float z) {
   if (act == kRelu) return z > 0.f || z != z ? z : 0.f;
-  if (act == kGelu) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-  if (act == kSilu) return z * sigmoid(z);
+  if (act == kGelu) {
+    float g;
+    return sizeof(T) == 4 ? 0.5f * z * (1.f + erff(z * 0.70710678118654752f)) : z * hastings(z, g);
+  }
+  if (act == kSilu) return z * sigmoid<T>(z);
   return z;
 }
-__device__ __forceinline__ float act_slope(uint32_t act, float z) {
+template <class T> __device__ __forceinline__ float act_slope(uint32_t act, float z) {
   if (act == kRelu) return z > 0.f ? 1.f : 0.f;
-  if (act == kGelu) return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
+  if (act == kGelu) {
+    if (sizeof(T) == 4) return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
+    float g;
+    const float phi = hastings(z, g);
+    return fmaf(z * 0.39894228040143268f, g, phi);
+  }
   if (act == kSilu) {
-    const float s = sigmoid(z);
+    const float s = sigmoid<T>(z);
     return s * (1.f + z * (1.f - s));
   }
   return 1.f;
 }
 
-__device__ __forceinline__ uint64_t drop_bits(const Drop& d, uint64_t row, uint32_t cols, uint32_t col) {
-  return draw(d.key, d.counter + row * ((cols + 3) / 4) + col / 4);
-}
-// A dropped element is zero whatever it was.
-__device__ __forceinline__ void drop4(const Drop& d, uint64_t bits, float (&v)[4]) {
+// N / 4 draws' bits on N elements; draw_at: the first draw's number plus 1, times the generator's step, plus the key.  A dropped element is
+// zero whatever it was.
+template <int N>
+__device__ __forceinline__ void drop_n(const Drop& d, uint64_t draw_at, float (&v)[N]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = ((uint32_t)(bits >> (16 * i)) & 0xFFFFu) >= d.q ? v[i] * d.scale : 0.f;
+  for (int g = 0; g < N / 4; ++g) {
+    const uint64_t bits = mix64(draw_at + kGamma * (uint64_t)g);
+    const uint32_t lo = (uint32_t)bits, hi = (uint32_t)(bits >> 32);
+    const uint32_t w[4] = {lo & 0xFFFFu, lo >> 16, hi & 0xFFFFu, hi >> 16};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[4 * g + i] = w[i] >= d.q ? v[4 * g + i] * d.scale : 0.f;
+  }
+}
+__device__ __forceinline__ uint64_t drop_at(const Drop& d, uint64_t row, uint32_t cols, uint32_t col) {
+  return d.key + kGamma * (d.counter + row * ((cols + 3) / 4) + col / 4 + 1);
 }
 
 // x as three bf16 values whose sum is x to 24 bits: the upper 8 bits cut off, so that they cannot overflow, the rest to nearest.
@@ -93,22 +171,51 @@ __device__ __forceinline__ void three_parts(float x, uint16_t& h, uint16_t& m, u
   l = __bfloat16_as_ushort(__float2bfloat16_rn(r - __bfloat162float(rm)));
 }
 
-// Four pre-activations (the bias is in them) of row `row`, columns col .. col + n - 1 of an array with `cols` columns.
+// N neighbouring values (a multiple of four) in three parts to planes `plane` elements apart.
+template <int N>
+__device__ __forceinline__ void store_parts(uint16_t* to, size_t plane, const float (&v)[N]) {
+#pragma unroll
+  for (int g = 0; g < N; g += 4) {
+    uint16_t h[4], m[4], l[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) three_parts(v[g + i], h[i], m[i], l[i]);
+    *reinterpret_cast<uint2*>(to + g) = make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
+    *reinterpret_cast<uint2*>(to + plane + g) = make_uint2(m[0] | (uint32_t)m[1] << 16, m[2] | (uint32_t)m[3] << 16);
+    *reinterpret_cast<uint2*>(to + 2 * plane + g) = make_uint2(l[0] | (uint32_t)l[1] << 16, l[2] | (uint32_t)l[3] << 16);
+  }
+}
+
+// Four pre-activations (the bias is in them) of row `row`, columns col .. col + n - 1 of an array with `cols` columns, and the residual there.
 template <class Out>
-__device__ __forceinline__ void finish4(const Epilogue& e, size_t row, uint32_t col, uint32_t cols, int n, float (&v)[4]) {
-  if (e.pre) store4(static_cast<Out*>(e.pre) + row * e.ld_pre + col, e.vec, n, v);
+__device__ __forceinline__ void finish4(const Epilogue& e, size_t row, uint32_t col, uint32_t cols, int n, float (&v)[4], const float (&residual)[4]) {
+  if (e.pre) store_n<Out, 4>(static_cast<Out*>(e.pre) + row * e.ld_pre + col, e.vec && n == 4, n, v);
   if (e.act) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = activate(e.act, v[i]);
+    for (int i = 0; i < 4; ++i) v[i] = activate<Out>(e.act, v[i]);
   }
-  if (e.drop.q) drop4(e.drop, drop_bits(e.drop, row, cols, col), v);
-  if (e.residual) {
-    float r[4];
-    load4(static_cast<const Out*>(e.residual) + row * e.ld_res + col, e.vec, n, r);
+  if (e.drop.q) drop_n<4>(e.drop, drop_at(e.drop, row, cols, col), v);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] += r[i];
+  for (int i = 0; i < 4; ++i) v[i] += residual[i];
+  store_n<Out, 4>(static_cast<Out*>(e.out) + row * e.ld_out + col, e.vec && n == 4, n, v);
+}
+template <class Out>
+__device__ __forceinline__ void finish4(const Epilogue& e, size_t row, uint32_t col, uint32_t cols, int n, float (&v)[4]) {
+  float r[4] = {};
+  if (e.residual) load_n<Out, 4>(static_cast<const Out*>(e.residual) + row * e.ld_res + col, e.vec && n == 4, n, r);
+  finish4<Out>(e, row, col, cols, n, v, r);
+}
+
+// Four sums of a product, the bias not in them yet.
+template <class Out>
+__device__ __forceinline__ void with_bias(const Product& p, uint32_t row, uint32_t col, float (&v)[4]) {
+  const int n = (int)min(4u, p.n - col);
+  if (p.e.bias) {
+    float b[4];
+    load4(p.e.bias_type, p.e.bias, col, false, n, b);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] += b[i];
   }
-  store4(static_cast<Out*>(e.out) + row * e.ld_out + col, e.vec, n, v);
+  finish4<Out>(p.e, row, col, p.n, n, v);
 }
 
 }  // namespace layer

@@ -17,18 +17,6 @@ namespace {
 
 constexpr int kTile = 64, kStep = 16, kThreads = 256, kLd = kTile + 4;
 
-template <class Out>
-__device__ __forceinline__ void with_bias(const Product& p, uint32_t row, uint32_t col, float (&v)[4]) {
-  const int n = (int)min(4u, p.n - col);
-  if (p.e.bias) {
-    float b[4];
-    load4(p.e.bias_type, p.e.bias, col, false, n, b);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] += b[i];
-  }
-  finish4<Out>(p.e, row, col, p.n, n, v);
-}
-
 template <class T, class Out>
 __global__ void __launch_bounds__(kThreads) product_fma_kernel(const Product p, const uint32_t tiles_n) {
   __shared__ __align__(16) float as[2][kStep][kLd], bs[2][kStep][kLd];

@@ -1,13 +1,13 @@
 // Large products of the dense layer on the 5th-generation tensor cores: C = A B, sums in tensor memory, through the layer's epilogue.
 //
 // One persistent CTA per SM (or a pair of CTAs on two) walks over output tiles of 128 rows a CTA and BN columns.  One thread feeds a
-// ring of stages by TMA (64 of k each, 128-byte swizzle), one issues tcgen05.mma, eight warps take finished sums out of tensor memory
+// ring of stages by TMA (64 of k each, 128-byte swizzle), one issues tcgen05.mma, the others take finished sums out of tensor memory
 // through a transposing buffer, so that rows are stored in whole sectors, while the next tile's products run into the other half of
 // tensor memory.  Either operand may be laid out along k or across it: TMA brings 64 x 64 blocks either way and the matrix
 // descriptors say which, so that the gradients' transposed products read the tensors as they are.
 //
 // PLANES 3: fp32 operands as three bf16 parts of 8 bits and more each (launch_planes), six products of parts per k; what is left out is
-// below 2^-24 of a product.  Tensor cores cut the sums they form, so sums of 128 of k leave tensor memory and are added up in fp32
+// below 2^-24 of a product.  Tensor cores cut the sums they form, so sums of 256 of k leave tensor memory and are added up in fp32
 // registers.  A stage then holds the three parts of both operands: each part is loaded once for the products it takes part in.
 //
 // Few tiles and a long k: k is split, the parts' sums go to the workspace and a second kernel adds them up in their order.
@@ -26,17 +26,23 @@ namespace aet {
 namespace layer {
 namespace {
 
-constexpr int kBK = 64, kThreads = 320, kEpiWarps = 8;
+constexpr int kBlock = 16;         // columns that go through a warp's buffer at once
+
 constexpr uint32_t kWaitLimit = 1u << 22;
-constexpr int kChunkBlocks = 2;    // PLANES 3: k blocks per sum in tensor memory
-constexpr uint32_t kGroup = 8;     // tile rows that are walked together, so that their operands meet in L2
+constexpr int kChunk = 256;         // PLANES 3: of k per sum in tensor memory
+constexpr uint32_t kGroup = 16;     // tile rows that are walked together, so that their operands meet in L2
 
 template <int PLANES, int BN, int CG>
 struct Ring {
+  static constexpr int bk = PLANES == 1 ? 64 : 32;     // of k in a stage
   static constexpr int b_rows = BN / CG;
-  static constexpr int a_part = 128 * kBK * 2, b_part = b_rows * kBK * 2;
+  static constexpr int a_part = 128 * bk * 2, b_part = b_rows * bk * 2, mn_block = 64 * bk * 2;
   static constexpr int a_bytes = PLANES * a_part, stage = a_bytes + PLANES * b_part;
-  static constexpr int trans = kEpiWarps * 32 * 32 * 4, rest = 512;
+  // warps that store: four to a quarter of tensor memory, since they wait for memory most of the time; fp32 sums in registers leave room
+  // for two (sixteen registers a thread and column block)
+  static constexpr int epi_warps = PLANES == 1 ? 16 : 8, threads = 64 + 32 * epi_warps;
+  static constexpr int cols = BN / (epi_warps / 4);     // columns a warp takes
+  static constexpr int trans = epi_warps * 32 * kBlock * 4, rest = 512;
   static constexpr int fit = (232448 - 1024 - trans - rest) / stage;
   static constexpr int stages = fit < 6 ? fit : 6;
   static constexpr int total = 1024 + stages * stage + trans + rest;
@@ -113,25 +119,29 @@ __device__ __forceinline__ void tmem_free(uint32_t at, uint32_t cols) {
   if (CG == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(cols));
   else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(cols));
 }
-__device__ __forceinline__ void tmem_ld32(uint32_t at, float (&v)[32]) {
-  uint32_t r[32];
+// 16 columns of the warp's rows; they are there after tmem_wait.
+__device__ __forceinline__ void tmem_ld(uint32_t at, uint32_t (&r)[kBlock]) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
       : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
-        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
-        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
       : "r"(at));
+}
+template <int N>
+__device__ __forceinline__ void tmem_wait(uint32_t (&r)[N][kBlock]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+  for (int c = 0; c < N; ++c)
+#pragma unroll
+    for (int i = 0; i < kBlock; ++i) asm volatile("" : "+r"(r[c][i]));     // (no use of a value moves in front of the wait)
 }
-// Matrix descriptor of a 128-byte-swizzled tile.  Along k: 8-row groups 1,024 bytes apart.  Across k: blocks of 64 rows (of M or N)
-// by 64 of k, 8,192 bytes apart, in them 8 of k every 1,024 bytes.
+// Matrix descriptor of a swizzled tile.  Along k: rows of bk elements (128 or 64 bytes, swizzled as wide), 8-row groups one after another.
+// Across k: 128-byte rows of 64 of M or N, bk of them to a block, blocks one after another, in them 8 of k every 1,024 bytes.
+template <int bk>
 __device__ __forceinline__ uint64_t tile_desc(uint32_t addr, bool mn) {
-  return (uint64_t)((addr & 0x3FFFF) >> 4) | (uint64_t)(mn ? 8192 >> 4 : 1) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+  const uint32_t lead = mn ? 64 * bk * 2 : 16, stride = mn || bk == 64 ? 1024 : 512;
+  const uint64_t swizzle = mn || bk == 64 ? 2 : 4;
+  return (uint64_t)((addr & 0x3FFFF) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(stride >> 4) << 32 | (uint64_t)1 << 46 | swizzle << 61;
 }
 
 struct Tile { uint32_t m, n, kb0, kb1, split; };
@@ -148,35 +158,53 @@ __device__ __forceinline__ Tile tile_of(const Launch& L, uint32_t item, uint32_t
   return t;
 }
 
-// 32 columns of 32 rows, a row per lane, through the warp's buffer to eight lanes a row; then the epilogue (or the workspace).
-template <class Out>
-__device__ __forceinline__ void store_block(const Launch& L, uint32_t split, float4* buf, int lane, const float* v, uint32_t m0, uint32_t n0) {
+// What a lane needs of a block of 32 rows and 16 columns besides the sums: four columns (lane mod 4) of the bias, and of the residual in
+// four rows (lane / 4 + 8 i).  Asked for before the sums are there.
+template <class Out> struct Ahead {
+  float res[4][4];
+  float bias[4];
+  __device__ __forceinline__ void ask(const Launch& L, int lane, uint32_t m0, uint32_t n0) {
+    const Epilogue& e = L.p.e;
+    const uint32_t col = n0 + 4 * (lane & 3);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) buf[lane * 8 + (j ^ (lane & 7))] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+    for (int i = 0; i < 4; ++i) bias[i] = 0.f;
+    if (L.splits > 1 || col >= L.p.n) return;
+    const int n = (int)min(4u, L.p.n - col);
+    if (e.bias) load4(e.bias_type, e.bias, col, false, n, bias);
+    if (!e.residual) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t row = m0 + 8 * i + lane / 4;
+      if (row >= L.p.m) continue;
+      const Out* r = static_cast<const Out*>(e.residual) + row * e.ld_res + col;
+      load_n<Out, 4>(r, e.vec && n == 4, n, res[i]);
+    }
+  }
+};
+// A block of sums, a row per lane, through the warp's buffer to four lanes a row; then the epilogue (or the workspace).
+template <class Out>
+__device__ __forceinline__ void store_block(const Launch& L, uint32_t split, float4* buf, int lane, const float (&v)[kBlock], const Ahead<Out>& ahead,
+                                            uint32_t m0, uint32_t n0) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) buf[lane * 4 + (j ^ (lane >> 1 & 3))] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
   __syncwarp();
   const Product& p = L.p;
-  const int j = lane & 7;
+  const int j = lane & 3;
   const uint32_t col = n0 + 4 * j;
   if (col < p.n) {
-    if (L.splits > 1) {
-#pragma unroll 4
-      for (int i = 0; i < 8; ++i) {
-        const int r = 4 * i + lane / 8;
-        if (m0 + r < p.m)
-          *reinterpret_cast<float4*>(L.partial + ((size_t)split * p.m + m0 + r) * L.ld_partial + col) = buf[r * 8 + (j ^ (r & 7))];
-      }
-    } else {
-      const int n = (int)min(4u, p.n - col);
-      float b[4] = {};
-      if (p.e.bias) load4(p.e.bias_type, p.e.bias, col, false, n, b);
-#pragma unroll 4
-      for (int i = 0; i < 8; ++i) {
-        const int r = 4 * i + lane / 8;
-        if (m0 + r < p.m) {
-          const float4 q = buf[r * 8 + (j ^ (r & 7))];
-          float z[4] = {q.x + b[0], q.y + b[1], q.z + b[2], q.w + b[3]};
-          finish4<Out>(p.e, m0 + r, col, p.n, n, z);
-        }
+    const int n = (int)min(4u, p.n - col);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = 8 * i + lane / 4;
+      if (m0 + r >= p.m) continue;
+      const float4 q = buf[r * 4 + (j ^ (r >> 1 & 3))];
+      if (L.splits > 1) {
+        *reinterpret_cast<float4*>(L.partial + ((size_t)split * p.m + m0 + r) * L.ld_partial + col) = q;
+      } else {
+        float z[4] = {q.x + ahead.bias[0], q.y + ahead.bias[1], q.z + ahead.bias[2], q.w + ahead.bias[3]}, res[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) res[k] = p.e.residual ? ahead.res[i][k] : 0.f;
+        finish4<Out>(p.e, m0 + r, col, p.n, n, z, res);
       }
     }
   }
@@ -184,7 +212,7 @@ __device__ __forceinline__ void store_block(const Launch& L, uint32_t split, flo
 }
 
 template <class Out, int PLANES, int BN, int CG>
-__global__ void __launch_bounds__(kThreads, 1) product_mma_kernel(const __grid_constant__ Launch L, const __grid_constant__ CUtensorMap map_a,
+__global__ void __launch_bounds__((Ring<PLANES, BN, CG>::threads), 1) product_mma_kernel(const __grid_constant__ Launch L, const __grid_constant__ CUtensorMap map_a,
                                                                   const __grid_constant__ CUtensorMap map_b) {
   using R = Ring<PLANES, BN, CG>;
   extern __shared__ unsigned char raw[];
@@ -196,7 +224,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_mma_kernel(const __grid_c
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t rank = CG == 1 ? 0 : blockIdx.x % CG;   // of the pair; the even CTA issues for both
   const uint32_t first = blockIdx.x / CG, step = gridDim.x / CG;
-  const uint32_t kbs = (L.p.k + kBK - 1) / kBK, items = L.tiles_m * L.tiles_n * L.splits;
+  const uint32_t kbs = (L.p.k + R::bk - 1) / R::bk, items = L.tiles_m * L.tiles_n * L.splits;
   constexpr uint32_t kCols = 2 * BN;
 
   if (threadIdx.x == 0) {
@@ -206,7 +234,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_mma_kernel(const __grid_c
     }
     for (int b = 0; b < 2; ++b) {
       bar_init(acc_full + 8 * b, 1);
-      bar_init(acc_empty + 8 * b, kEpiWarps * CG);
+      bar_init(acc_empty + 8 * b, R::epi_warps * CG);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -234,19 +262,19 @@ __global__ void __launch_bounds__(kThreads, 1) product_mma_kernel(const __grid_c
           const uint32_t bar = CG == 1 ? full + 8 * s : in_cta(full + 8 * s, 0);
           if (rank == 0) bar_expect(full + 8 * s, R::stage * CG);
           const uint32_t at = base + s * R::stage;
-          const int k0 = (int)(kb * kBK);
+          const int k0 = (int)(kb * R::bk);
 #pragma unroll
           for (int q = 0; q < PLANES; ++q) {
             const uint32_t a = at + q * R::a_part, b = at + R::a_bytes + q * R::b_part;
             if (L.a_mn) {
               tma_load<CG>(a, &map_a, bar, m0, k0, q);
-              tma_load<CG>(a + 8192, &map_a, bar, m0 + 64, k0, q);
+              tma_load<CG>(a + R::mn_block, &map_a, bar, m0 + 64, k0, q);
             } else {
               tma_load<CG>(a, &map_a, bar, k0, m0, q);
             }
             if (L.b_mn) {
 #pragma unroll
-              for (int c = 0; c < R::b_rows / 64; ++c) tma_load<CG>(b + c * 8192, &map_b, bar, n0 + c * 64, k0, q);
+              for (int c = 0; c < R::b_rows / 64; ++c) tma_load<CG>(b + c * R::mn_block, &map_b, bar, n0 + c * 64, k0, q);
             } else {
               tma_load<CG>(b, &map_b, bar, k0, n0, q);
             }
@@ -265,7 +293,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_mma_kernel(const __grid_c
       for (uint32_t item = first; item < items && ok; item += step) {
         const Tile t = tile_of(L, item, kbs);
         for (uint32_t kb = t.kb0; kb < t.kb1 && ok; ++ac) {
-          const uint32_t end = PLANES == 1 ? t.kb1 : min(kb + kChunkBlocks, t.kb1);
+          const uint32_t end = PLANES == 1 ? t.kb1 : min(kb + kChunk / R::bk, t.kb1);
           const uint32_t d = tmem + (ac & 1) * BN;
           ok = bar_wait(acc_empty + 8 * (ac & 1), (ac >> 1 & 1) ^ 1);
           if (!ok) break;
@@ -277,10 +305,10 @@ __global__ void __launch_bounds__(kThreads, 1) product_mma_kernel(const __grid_c
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t at = base + s * R::stage;
-            const uint64_t da = tile_desc(at, L.a_mn), db = tile_desc(at + R::a_bytes, L.b_mn);
+            const uint64_t da = tile_desc<R::bk>(at, L.a_mn), db = tile_desc<R::bk>(at + R::a_bytes, L.b_mn);
             if (PLANES == 1) {
 #pragma unroll
-              for (int k = 0; k < kBK / 16; ++k) {
+              for (int k = 0; k < R::bk / 16; ++k) {
                 mma<CG>(d, da + k * a_step, db + k * b_step, L.idesc, accumulate);
                 accumulate = 1;
               }
@@ -290,7 +318,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_mma_kernel(const __grid_c
 #pragma unroll
               for (int q = 0; q < 6; ++q)
 #pragma unroll
-                for (int k = 0; k < kBK / 16; ++k) {
+                for (int k = 0; k < R::bk / 16; ++k) {
                   mma<CG>(d, da + pa[q] * (R::a_part >> 4) + k * a_step, db + pb[q] * (R::b_part >> 4) + k * b_step, L.idesc, accumulate);
                   accumulate = 1;
                 }
@@ -302,23 +330,29 @@ __global__ void __launch_bounds__(kThreads, 1) product_mma_kernel(const __grid_c
       }
     }
   } else {
-    const int ew = warp - 2, half = ew / 4;
+    const int ew = warp - 2, part = ew / 4;
     const uint32_t lanes = (uint32_t)(warp % 4) * 32;      // the quarter of tensor memory this warp may read
-    float4* buf = trans + ew * 256;
-    constexpr int kBlocks = BN / 64;                       // blocks of 32 columns: half of the tile's
+    float4* buf = trans + ew * (32 * kBlock / 4);
+    constexpr int kBlocks = R::cols / kBlock;
     uint32_t ac = 0;
     bool ok = true;
     for (uint32_t item = first; item < items; item += step) {
       const Tile t = tile_of(L, item, kbs);
-      const uint32_t m0 = t.m * (128 * CG) + rank * 128 + lanes, n0 = t.n * BN + half * (BN / 2);
-      const uint32_t at = tmem + (lanes << 16) + half * (BN / 2);
+      const uint32_t m0 = t.m * (128 * CG) + rank * 128 + lanes, n0 = t.n * BN + part * R::cols;
+      const uint32_t at = tmem + (lanes << 16) + part * R::cols;
+      Ahead<Out> ahead;
       if (PLANES == 1) {
+        ahead.ask(L, lane, m0, n0);
         if (ok) ok = bar_wait(acc_full + 8 * (ac & 1), ac >> 1 & 1);
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
         for (int c = 0; c < kBlocks; ++c) {
-          float v[32];
-          tmem_ld32(at + (ac & 1) * BN + c * 32, v);
+          uint32_t w[1][kBlock];
+          tmem_ld(at + (ac & 1) * BN + c * kBlock, w[0]);
+          tmem_wait(w);
+          float v[kBlock];
+#pragma unroll
+          for (int i = 0; i < kBlock; ++i) v[i] = __uint_as_float(w[0][i]);
           if (c == kBlocks - 1) {
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
@@ -326,26 +360,29 @@ __global__ void __launch_bounds__(kThreads, 1) product_mma_kernel(const __grid_c
           }
           if (!ok) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = CUDART_NAN_F;
+            for (int i = 0; i < kBlock; ++i) v[i] = CUDART_NAN_F;
           }
-          store_block<Out>(L, t.split, buf, lane, v, m0, n0 + c * 32);
+          store_block<Out>(L, t.split, buf, lane, v, ahead, m0, n0 + c * kBlock);
+          if (c + 1 < kBlocks) ahead.ask(L, lane, m0, n0 + (c + 1) * kBlock);
         }
         ++ac;
       } else {
-        float sum[kBlocks][32];
+        float sum[kBlocks][kBlock];
 #pragma unroll
         for (int c = 0; c < kBlocks; ++c)
 #pragma unroll
-          for (int i = 0; i < 32; ++i) sum[c][i] = 0.f;
-        for (uint32_t kb = t.kb0; kb < t.kb1; kb += kChunkBlocks, ++ac) {
+          for (int i = 0; i < kBlock; ++i) sum[c][i] = 0.f;
+        for (uint32_t kb = t.kb0; kb < t.kb1; kb += kChunk / R::bk, ++ac) {
           if (ok) ok = bar_wait(acc_full + 8 * (ac & 1), ac >> 1 & 1);
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
-          for (int c = 0; c < kBlocks; ++c) {
-            float v[32];
-            tmem_ld32(at + (ac & 1) * BN + c * 32, v);
+          for (int c = 0; c < kBlocks; c += 2) {
+            uint32_t w[2][kBlock];
+            tmem_ld(at + (ac & 1) * BN + c * kBlock, w[0]);
+            tmem_ld(at + (ac & 1) * BN + (c + 1) * kBlock, w[1]);
+            tmem_wait(w);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) sum[c][i] += v[i];
+            for (int i = 0; i < kBlock; ++i) sum[c][i] += __uint_as_float(w[0][i]), sum[c + 1][i] += __uint_as_float(w[1][i]);
           }
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
           __syncwarp();
@@ -355,9 +392,10 @@ __global__ void __launch_bounds__(kThreads, 1) product_mma_kernel(const __grid_c
         for (int c = 0; c < kBlocks; ++c) {
           if (!ok) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) sum[c][i] = CUDART_NAN_F;
+            for (int i = 0; i < kBlock; ++i) sum[c][i] = CUDART_NAN_F;
           }
-          store_block<Out>(L, t.split, buf, lane, sum[c], m0, n0 + c * 32);
+          ahead.ask(L, lane, m0, n0 + c * kBlock);
+          store_block<Out>(L, t.split, buf, lane, sum[c], ahead, m0, n0 + c * kBlock);
         }
       }
     }
@@ -405,27 +443,26 @@ __global__ void __launch_bounds__(256) planes_kernel(const T* src, size_t ld, ui
   const uint32_t col = (uint32_t)(g % per) * 8;
   const T* s = src + row * ld + col;
   uint16_t* d = dst + row * ld_dst + col;
+  const bool whole = col + 8 <= cols && (uintptr_t)s % 16 == 0;
   if (kPlanes == 1) {
-    Pack<uint16_t, 8> v;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v.v[i] = col + i < cols ? reinterpret_cast<const uint16_t*>(s)[i] : (uint16_t)0;
-    *reinterpret_cast<Pack<uint16_t, 8>*>(d) = v;
-  } else {
-    Pack<uint16_t, 8> v[3];
-    float x[8];
-    const bool whole = col + 8 <= cols;
-    if (whole && (uintptr_t)s % 16 == 0) {
-      const Pack<float, 4> lo = *reinterpret_cast<const Pack<float, 4>*>(s), hi = *reinterpret_cast<const Pack<float, 4>*>(s + 4);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = lo.v[i], x[4 + i] = hi.v[i];
+    uint4 v;
+    if (whole) {
+      v = *reinterpret_cast<const uint4*>(s);
     } else {
+      const uint16_t* q = reinterpret_cast<const uint16_t*>(s);
+      uint32_t w[4];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = col + i < cols ? to_f32(s[i]) : 0.f;
+      for (int i = 0; i < 4; ++i) w[i] = (col + 2 * i < cols ? q[2 * i] : 0u) | (col + 2 * i + 1 < cols ? (uint32_t)q[2 * i + 1] : 0u) << 16;
+      v = make_uint4(w[0], w[1], w[2], w[3]);
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) three_parts(x[i], v[0].v[i], v[1].v[i], v[2].v[i]);
-#pragma unroll
-    for (int q = 0; q < 3; ++q) *reinterpret_cast<Pack<uint16_t, 8>*>(d + q * plane) = v[q];
+    *reinterpret_cast<uint4*>(d) = v;
+  } else {
+    float x[2][4];
+    const float* f = reinterpret_cast<const float*>(s);
+    load_n<float, 4>(f, whole, col < cols ? (int)min(4u, cols - col) : 0, x[0]);
+    load_n<float, 4>(f + 4, whole, col + 4 < cols ? (int)min(4u, cols - col - 4) : 0, x[1]);
+    store_parts<4>(d, plane, x[0]);
+    store_parts<4>(d + 4, plane, x[1]);
   }
 }
 
@@ -443,14 +480,15 @@ Encode encoder() {
   return reinterpret_cast<Encode>(f);
 }
 
-// [planes][outer][inner] elements, boxes of 64 x box_rows.
-cudaError_t encode(CUtensorMap* map, const MmaOperand& o, uint32_t type, uint32_t planes, uint64_t inner, uint64_t outer, uint32_t box_rows) {
+// [planes][outer][inner] elements, boxes of box_cols x box_rows.
+cudaError_t encode(CUtensorMap* map, const MmaOperand& o, uint32_t type, uint32_t planes, uint64_t inner, uint64_t outer, uint32_t box_cols, uint32_t box_rows) {
   const Encode f = encoder();
   if (!f) return cudaErrorNotSupported;
   const cuuint64_t dims[3] = {inner, outer, planes}, strides[2] = {o.ld * 2, (planes > 1 ? o.plane : (outer * o.ld + 7) / 8 * 8) * 2};
-  const cuuint32_t box[3] = {64, box_rows, 1}, steps[3] = {1, 1, 1};
+  const cuuint32_t box[3] = {box_cols, box_rows, 1}, steps[3] = {1, 1, 1};
   const CUresult r = f(map, type == kF16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(o.p), dims, strides, box, steps,
-                       CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                       CU_TENSOR_MAP_INTERLEAVE_NONE, box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                       CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
@@ -467,8 +505,9 @@ cudaError_t run(const MmaProduct& m, cudaStream_t s) {
   const uint32_t format = m.type == kF16 ? 0 : 1;
   L.idesc = (1u << 4) | (format << 7) | (format << 10) | (L.a_mn << 15) | (L.b_mn << 16) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(128 * CG >> 4) << 24);
   CUtensorMap ma, mb;
-  cudaError_t e = L.a_mn ? encode(&ma, m.a, m.type, PLANES, m.p.m, m.p.k, 64) : encode(&ma, m.a, m.type, PLANES, m.p.k, m.p.m, 128);
-  if (e == cudaSuccess) e = L.b_mn ? encode(&mb, m.b, m.type, PLANES, m.p.n, m.p.k, 64) : encode(&mb, m.b, m.type, PLANES, m.p.k, m.p.n, R::b_rows);
+  cudaError_t e = L.a_mn ? encode(&ma, m.a, m.type, PLANES, m.p.m, m.p.k, 64, R::bk) : encode(&ma, m.a, m.type, PLANES, m.p.k, m.p.m, R::bk, 128);
+  if (e == cudaSuccess)
+    e = L.b_mn ? encode(&mb, m.b, m.type, PLANES, m.p.n, m.p.k, 64, R::bk) : encode(&mb, m.b, m.type, PLANES, m.p.k, m.p.n, R::bk, R::b_rows);
   if (e != cudaSuccess) return e;
   const auto kernel = product_mma_kernel<Out, PLANES, BN, CG>;
   e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, R::total);
@@ -479,7 +518,7 @@ cudaError_t run(const MmaProduct& m, cudaStream_t s) {
   const uint32_t items = L.tiles_m * L.tiles_n * L.splits;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((items < slots ? items : slots) * CG);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(R::threads);
   cfg.dynamicSmemBytes = R::total;
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
@@ -510,7 +549,7 @@ MmaShape mma_shape(uint32_t planes, uint32_t m, uint32_t n, uint32_t k) {
   const uint64_t pairs = (uint64_t)((m + 255) / 256) * ((n + 255) / 256);
   r.pair = pairs >= 74;
   const uint64_t tiles = r.pair ? pairs : (uint64_t)((m + 127) / 128) * ((n + 127) / 128), slots = r.pair ? 74 : 148;
-  const uint64_t kbs = (k + kBK - 1) / kBK;
+  const uint64_t kbs = (k + 63) / 64;
   uint64_t splits = slots / tiles;                       // as many parts as there are SMs left, each with 256 of k and more
   if (splits > kbs / 4) splits = kbs / 4;
   if (splits > 32) splits = 32;

@@ -44,6 +44,10 @@ struct Product {
 // Small products: 64 x 64 tiles on FMAs, k split over the CTAs of a cluster.
 cudaError_t launch_product_fma(const Product& p, cudaStream_t s);
 
+// Up to eight rows of A along k against a B across it (see layer_rows_kernel.cu).
+bool rows_kernel_takes(uint32_t m, uint32_t k);
+cudaError_t launch_product_rows(const Product& p, cudaStream_t s);
+
 // Large products (see layer_mma_kernel.cu).  An operand of a tensor-core product: 16-bit elements, rows `ld` elements apart and from
 // 16-byte boundaries on, `planes` of them `plane` elements apart (three: the parts of fp32); mn: its rows run along k, not across.
 struct MmaOperand {
@@ -75,7 +79,8 @@ struct SlopeLaunch {
   const void *dy, *pre;   // pre null: act is none
   void *dz, *db;          // db null: no sums
   size_t ld_dy, ld_pre, ld_dz, plane;
-  uint32_t type, db_type, act, accumulate;   // accumulate: db += sums
+  uint32_t type, db_type, act, accumulate;   // of dy and pre; accumulate: db += sums
+  uint32_t dz_bf16;       // dz is bf16 where dy is fp32
   uint32_t rows, cols;
   Drop drop;
   float* partial;         // slope_partial_floats() of workspace

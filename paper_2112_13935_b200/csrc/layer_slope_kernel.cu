@@ -1,66 +1,84 @@
 // What the gradient of a dense layer starts with: dz = drop(dy) act'(pre), and the sums of dz over the rows (the bias's gradient).
 //
-// One pass over dy and pre, bound by memory.  A CTA takes a slab of rows and 128 columns, a thread four neighbouring columns (one
-// draw of the dropout generator, one 8- or 16-byte access); the sums of a slab go to the workspace and a second small kernel adds
-// the slabs up in their order, so that they are the same from call to call.
+// One pass over dy and pre, bound by memory.  A thread keeps 16 bytes of columns and goes down a slab of rows, two at a time with all
+// their loads under way; the sums of a slab go to the workspace and a second small kernel adds the slabs up in their order, so that
+// they are the same from call to call.
 #include <cuda_runtime.h>
 
-#include "layer_common.cuh"
+#include "layer_rows.cuh"
 
 namespace aet {
 namespace layer {
 namespace {
 
-constexpr int kLanes = 32, kRowLanes = 8, kCols = 4 * kLanes;
+constexpr int kThreads = 256, kRows = 2;
 
-template <class T>
-__global__ void __launch_bounds__(kLanes* kRowLanes) slope_kernel(const SlopeLaunch p, const uint32_t slabs, const bool vec) {
-  __shared__ __align__(16) float sums[kRowLanes][kCols];
-  const int lane = threadIdx.x % kLanes, rl = threadIdx.x / kLanes;
-  const uint32_t blocks = (p.cols + kCols - 1) / kCols;
-  const uint32_t slab = blockIdx.x / blocks, col = blockIdx.x % blocks * kCols + lane * 4;
-  const uint64_t r0 = (uint64_t)p.rows * slab / slabs, r1 = (uint64_t)p.rows * (slab + 1) / slabs;
-  const int n = col < p.cols ? (int)min(4u, p.cols - col) : 0;
+template <class T, int N, bool kVec>
+__global__ void __launch_bounds__(kThreads, 4) slope_kernel(const SlopeLaunch p, const uint32_t slabs, const uint32_t log) {
+  __shared__ __align__(16) float sums[kThreads * N];
+  const uint32_t lane = threadIdx.x & ((1u << log) - 1), down = threadIdx.x >> log, at_once = kThreads >> log;
+  const uint32_t col = ((blockIdx.x << log) + lane) * N;
+  const size_t r_from = (size_t)p.rows * blockIdx.y / slabs, r_to = (size_t)p.rows * (blockIdx.y + 1) / slabs;
+  const int n = col < p.cols ? (int)min((uint32_t)N, p.cols - col) : 0;
+  const bool whole = kVec && n == N;
   const T* dy = static_cast<const T*>(p.dy);
   const T* pre = static_cast<const T*>(p.pre);
-  float acc[4] = {};
+  float acc[N] = {};
   if (n) {
-#pragma unroll 4
-    for (uint64_t r = r0 + rl; r < r1; r += kRowLanes) {
-      float v[4];
-      load4(dy + r * p.ld_dy + col, vec, n, v);
-      if (p.drop.q) drop4(p.drop, drop_bits(p.drop, r, p.cols, col), v);
-      if (pre) {
-        float z[4];
-        load4(pre + r * p.ld_pre + col, vec, n, z);
+    for (size_t r0 = r_from + down; r0 < r_to; r0 += (size_t)kRows * at_once) {
+      Words<T, N> q[kRows], w[kRows];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float f = act_slope(p.act, z[i]);
-          v[i] = p.act == kRelu ? (f != 0.f ? v[i] : 0.f) : v[i] * f;
+      for (int i = 0; i < kRows; ++i) {
+        const size_t r = r0 + (size_t)i * at_once;
+        if (r >= r_to) break;
+        q[i] = load_words<T, N>(dy + r * p.ld_dy + col, whole, n);
+        if (pre) w[i] = load_words<T, N>(pre + r * p.ld_pre + col, whole, n);
+      }
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) {
+        const size_t r = r0 + (size_t)i * at_once;
+        if (r >= r_to) break;
+        keep_words(q[i]);
+        float v[N];
+        unpack<T, N>(q[i], v);
+        if (p.drop.q) drop_n<N>(p.drop, drop_at(p.drop, r, p.cols, col), v);
+        if (pre) {
+          keep_words(w[i]);
+          float z[N];
+          unpack<T, N>(w[i], z);
+          if (p.act == kRelu) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[k] = z[k] > 0.f ? v[k] : 0.f;
+          } else if (p.act == kGelu) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[k] *= act_slope<T>(kGelu, z[k]);
+          } else {
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[k] *= act_slope<T>(kSilu, z[k]);
+          }
         }
+        if (p.dz && p.plane) {
+          store_parts<N>(static_cast<uint16_t*>(p.dz) + r * p.ld_dz + col, p.plane, v);   // (0 past the last column)
+        } else if (p.dz && p.dz_bf16) {
+          store_n<__nv_bfloat16, N>(static_cast<__nv_bfloat16*>(p.dz) + r * p.ld_dz + col, whole, n, v);
+        } else if (p.dz) {
+          store_n<T, N>(static_cast<T*>(p.dz) + r * p.ld_dz + col, whole, n, v);
+        }
+#pragma unroll
+        for (int k = 0; k < N; ++k) acc[k] += v[k];
       }
-      if (p.dz && p.plane) {
-        Pack<uint16_t, 4> q[3] = {};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) three_parts(v[i], q[0].v[i], q[1].v[i], q[2].v[i]);   // (0 past the last column)
-        uint16_t* d = static_cast<uint16_t*>(p.dz) + r * p.ld_dz + col;
-#pragma unroll
-        for (int i = 0; i < 3; ++i) *reinterpret_cast<Pack<uint16_t, 4>*>(d + i * p.plane) = q[i];
-      } else if (p.dz) {
-        store4(static_cast<T*>(p.dz) + r * p.ld_dz + col, vec, n, v);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) acc[i] += v[i];
     }
   }
   if (!p.db) return;
-  *reinterpret_cast<float4*>(&sums[rl][lane * 4]) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+#pragma unroll
+  for (int k = 0; k < N; ++k) sums[(down << log) * N + k * (1u << log) + lane] = acc[k];
   __syncthreads();
-  const uint32_t c = blockIdx.x % blocks * kCols + threadIdx.x;
-  if (threadIdx.x < kCols && c < p.cols) {
+  for (uint32_t e = threadIdx.x; e < (uint32_t)N << log; e += kThreads) {
+    const uint32_t c = ((blockIdx.x << log) + (e & ((1u << log) - 1))) * N + (e >> log);
+    if (c >= p.cols) continue;
     float v = 0.f;
-    for (int q = 0; q < kRowLanes; ++q) v += sums[q][threadIdx.x];
-    p.partial[(size_t)slab * p.cols + c] = v;
+    for (uint32_t q = 0; q < at_once; ++q) v += sums[(q << log) * N + e];
+    p.partial[(size_t)blockIdx.y * p.cols + c] = v;
   }
 }
 
@@ -71,8 +89,10 @@ __global__ void __launch_bounds__(256) slab_sums_kernel(const float* partial, ui
   const int lane = threadIdx.x % 32, part = threadIdx.x / 32;
   const uint32_t c = blockIdx.x * 32 + lane;
   float v = 0.f;
-  if (c < cols)
+  if (c < cols) {
+#pragma unroll 8
     for (uint32_t q = part; q < slabs; q += 8) v += partial[(size_t)q * cols + c];
+  }
   sums[part][lane] = v;
   __syncthreads();
   if (part || c >= cols) return;
@@ -81,20 +101,31 @@ __global__ void __launch_bounds__(256) slab_sums_kernel(const float* partial, ui
   db[c] = from_f32<T>(v);
 }
 
+// Slabs for about eight CTAs on each of 148 SMs, each with two rows and more to a thread.  (By the narrowest columns a thread may keep,
+// so that the workspace does not hang on where the arrays start.)
 uint32_t slabs_of(uint32_t rows, uint32_t cols) {
-  const uint32_t blocks = (cols + kCols - 1) / kCols;
-  // about eight CTAs for each of 148 SMs, each with eight rows and more to a thread
-  const uint32_t want = (148 * 8 + blocks - 1) / blocks, most = (rows + 8 * kRowLanes - 1) / (8 * kRowLanes);
-  return want < most ? want : most ? most : 1;
+  const uint32_t log = log_lanes<4>(cols);
+  const uint64_t across = (((uint64_t)cols + 3) / 4 + (1u << log) - 1) >> log, at_once = (uint64_t)(kThreads >> log) * kRows;
+  const uint64_t want = (148 * 8 + across - 1) / across, most = (rows + at_once - 1) / at_once;
+  const uint64_t n = want < most ? want : most;
+  return n ? (uint32_t)n : 1;
 }
 
-bool aligned4(const void* p, size_t ld, size_t bytes) { return !p || ((uintptr_t)p % (4 * bytes) == 0 && ld % 4 == 0); }
+bool aligned(const void* p, size_t ld, size_t n, size_t bytes) { return !p || ((uintptr_t)p % (n * bytes) == 0 && ld % n == 0); }
 
+template <class T, int N, bool kVec>
+void go(const SlopeLaunch& p, uint32_t slabs, cudaStream_t s) {
+  const uint32_t log = log_lanes<N>(p.cols);
+  const uint64_t across = (((uint64_t)p.cols + N - 1) / N + (1u << log) - 1) >> log;
+  slope_kernel<T, N, kVec><<<dim3((unsigned)across, slabs), kThreads, 0, s>>>(p, slabs, log);
+}
 template <class T>
 cudaError_t run(const SlopeLaunch& p, cudaStream_t s) {
-  const uint32_t slabs = slabs_of(p.rows, p.cols), blocks = (p.cols + kCols - 1) / kCols;
-  const bool vec = aligned4(p.dy, p.ld_dy, sizeof(T)) && aligned4(p.pre, p.ld_pre, sizeof(T)) && aligned4(p.dz, p.ld_dz, sizeof(T));
-  slope_kernel<T><<<slabs * blocks, kLanes * kRowLanes, 0, s>>>(p, slabs, vec);
+  constexpr int N = 16 / (int)sizeof(T);
+  const uint32_t slabs = slabs_of(p.rows, p.cols);
+  const bool vec = aligned(p.dy, p.ld_dy, N, sizeof(T)) && aligned(p.pre, p.ld_pre, N, sizeof(T)) && (p.plane || aligned(p.dz, p.ld_dz, N, p.dz_bf16 ? 2 : sizeof(T)));
+  if (vec) go<T, N, true>(p, slabs, s);
+  else go<T, 4, false>(p, slabs, s);
   if (p.db) {
     const uint32_t grid = (p.cols + 31) / 32;
     if (p.db_type == kF32) slab_sums_kernel<<<grid, 256, 0, s>>>(p.partial, slabs, p.cols, static_cast<float*>(p.db), p.accumulate);

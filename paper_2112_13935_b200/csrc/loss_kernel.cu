@@ -12,8 +12,6 @@
 #include <cuda_runtime.h>
 #include <math_constants.h>
 
-#include <type_traits>
-
 #include "layer_common.cuh"
 
 namespace cg = cooperative_groups;
@@ -75,39 +73,6 @@ template <class T> struct Row {
   __device__ __forceinline__ bool ragged(int32_t q) const { return (q == 0 && shift) || (q == count - 1 && (n + shift) % kV<T>); }
   __device__ __forceinline__ bool mine(int32_t j) const { return j >= 0 && j < n; }
 };
-// (Words are taken apart and put together by hand: through an array of elements they would go to local memory.)
-template <class T> __device__ __forceinline__ void unpack(const uint4& q, float (&v)[kV<T>]) {
-  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (sizeof(T) == 4) {
-      v[i] = __uint_as_float(w[i]);
-    } else if constexpr (std::is_same<T, __half>::value) {
-      const float2 f = __half22float2(__halves2half2(__ushort_as_half((unsigned short)w[i]), __ushort_as_half((unsigned short)(w[i] >> 16))));
-      v[2 * i] = f.x;
-      v[2 * i + 1] = f.y;
-    } else {
-      v[2 * i] = __uint_as_float(w[i] << 16);
-      v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-    }
-  }
-}
-template <class T> __device__ __forceinline__ uint4 pack(const float (&v)[kV<T>]) {
-  uint32_t w[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (sizeof(T) == 4) {
-      w[i] = __float_as_uint(v[i]);
-    } else if constexpr (std::is_same<T, __half>::value) {
-      const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
-      w[i] = (uint32_t)__half_as_ushort(__low2half(h)) | (uint32_t)__half_as_ushort(__high2half(h)) << 16;
-    } else {
-      const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-      w[i] = (uint32_t)__bfloat16_as_ushort(__low2bfloat16(h)) | (uint32_t)__bfloat16_as_ushort(__high2bfloat16(h)) << 16;
-    }
-  }
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
 // Piece q of the row, where there is one (below `end`); what is not of the row is -inf.
 template <class T> __device__ __forceinline__ uint4 fetch(const Row<T>& r, int32_t q, int32_t end) {
   const uint32_t none = sizeof(T) == 4 ? 0xFF800000u : std::is_same<T, __half>::value ? 0xFC00FC00u : 0xFF80FF80u;
@@ -118,11 +83,11 @@ template <class T> __device__ __forceinline__ uint4 fetch(const Row<T>& r, int32
 template <class T> __device__ __forceinline__ void trim(const Row<T>& r, uint4& v, int32_t q) {
   if (!r.ragged(q)) return;
   float f[kV<T>];
-  unpack<T>(v, f);
+  unpack<T, kV<T>>(v, f);
 #pragma unroll
   for (int i = 0; i < kV<T>; ++i)
     if (!r.mine(q * kV<T> - r.shift + i)) f[i] = -CUDART_INF_F;
-  v = pack<T>(f);
+  v = pack<T, kV<T>>(f);
 }
 template <class T> __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {   // of the halves of a word; a NaN loses
   uint32_t r;
@@ -133,17 +98,17 @@ template <class T> __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t
 template <class T> __device__ __forceinline__ float largest(const uint4& v) {
   float f[kV<T>];
   if constexpr (sizeof(T) == 4) {
-    unpack<T>(v, f);
+    unpack<T, kV<T>>(v, f);
     return fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3]));
   } else {
     const uint32_t m = max2<T>(max2<T>(v.x, v.y), max2<T>(v.z, v.w));
-    unpack<T>(make_uint4(m, m, m, m), f);
+    unpack<T, kV<T>>(make_uint4(m, m, m, m), f);
     return fmaxf(f[0], f[1]);
   }
 }
 template <class T> __device__ __forceinline__ float powers(const uint4& v, const Base& b) {
   float f[kV<T>], sum = 0.f;
-  unpack<T>(v, f);
+  unpack<T, kV<T>>(v, f);
 #pragma unroll
   for (int k = 0; k < kV<T>; ++k) sum += exp2_of(fmaf(f[k], b.c, -b.t));
   return sum;
@@ -167,11 +132,11 @@ template <class T> struct Slope {
 template <class T> __device__ __forceinline__ void write_grad(const Row<T>& r, const uint4& q, int32_t at, const Slope<T>& s, bool whole) {
   const int32_t j = at * kV<T> - r.shift;
   float v[kV<T>];
-  unpack<T>(q, v);
+  unpack<T, kV<T>>(q, v);
 #pragma unroll
   for (int i = 0; i < kV<T>; ++i) v[i] = exp2_of(fmaf(v[i], s.b.c, -s.b.t)) * s.w;
   if (whole) {
-    __stcs(reinterpret_cast<uint4*>(s.g + j), pack<T>(v));
+    __stcs(reinterpret_cast<uint4*>(s.g + j), pack<T, kV<T>>(v));
   } else {
 #pragma unroll
     for (int i = 0; i < kV<T>; ++i)
@@ -191,7 +156,7 @@ __device__ __forceinline__ void write_loss(const LossLaunch& p, size_t row, cons
 template <class T> __device__ __forceinline__ void write_top(const LossLaunch& p, const Row<T>& r, size_t row, const Part& a, const uint4& q, int32_t at) {
   if (a.at != at || a.sum != a.sum) return;
   float v[kV<T>];
-  unpack<T>(q, v);
+  unpack<T, kV<T>>(q, v);
   int32_t first = kNone;
 #pragma unroll
   for (int i = kV<T> - 1; i >= 0; --i)

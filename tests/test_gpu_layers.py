@@ -65,6 +65,13 @@ def test_dense_forward_sizes(rows, n_in, n_out, type):
 
 
 @pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,n_in,n_out", [(1, 1, 1000), (1, 520, 8), (2, 16384, 70), (3, 5000, 2049), (8, 300, 1000), (8, 16384, 9), (1, 20000, 300), (7, 64, 20000)])
+@pytest.mark.parametrize("over", [dict(act="silu", pre=True), dict(pad=1, residual=True, rate=0.2), dict(pad=8, shift=1, residual=True, in_place=True)])
+def test_dense_forward_few_rows(rows, n_in, n_out, type, over):
+    check_forward(rows, n_in, n_out, type, **over)
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("over", [
     dict(act="none", bias=False), dict(act="gelu", residual=True), dict(act="silu", rate=0.3), dict(act="relu", rate=0.5, residual=True, pre=True),
     dict(pad=1, act="gelu", residual=True, pre=True), dict(pad=3, shift=1, rate=0.1, residual=True, pre=True), dict(pad=8, act="silu"),
@@ -307,7 +314,7 @@ def test_loss_of_odd_rows(n, type):
 # ---- dropout -------------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
-@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 3), (3, 4), (5, 9), (129, 1001), (64, 64), (700, 128), (2, 70000)])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 3), (3, 4), (5, 9), (129, 1001), (64, 64), (700, 128), (2, 70000), (30000, 12)])
 @pytest.mark.parametrize("over", [dict(rate=0.5), dict(rate=0.1, residual=True), dict(rate=0.0), dict(rate=0.9999, pad=1, shift=1, residual=True), dict(rate=0.3, pad=4, in_place="x"), dict(rate=0.3, residual=True, in_place="residual")])
 def test_dropout(rows, cols, type, over):
     t = lh.TYPES[type]
