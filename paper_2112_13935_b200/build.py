@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libaet_b200.so")
 SOURCES = ["aet_api.cu", "aet_schedule.cpp", "lr_kernel.cu", "lr_chain_kernel.cu", "lr_relay_kernel.cu", "lr_block_kernel.cu", "mlp_kernel.cu", "mlp_mma_kernel.cu", "mlp_wide_kernel.cu", "mlp_tc_kernel.cu", "cnn_kernel.cu", "cnn_mma_kernel.cu", "agg_kernel.cu", "no_alloc.cu",
-           "device_info.cu", "layer_api.cu", "layer_dense.cu", "evaluate.cu", "layer_fma_kernel.cu", "layer_mma_kernel.cu", "layer_rows_kernel.cu", "layer_slope_kernel.cu", "loss_kernel.cu", "dropout_kernel.cu"]
+           "device_info.cu", "layer_api.cu", "layer_dense.cu", "evaluate.cu", "layer_fma_kernel.cu", "layer_mma_kernel.cu", "layer_f32_kernel.cu", "layer_copy_kernel.cu", "layer_rows_kernel.cu", "layer_slope_kernel.cu", "loss_kernel.cu", "dropout_kernel.cu"]
 
 
 def _newest(paths):

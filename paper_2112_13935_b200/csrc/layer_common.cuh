@@ -46,6 +46,13 @@ __device__ __forceinline__ void unpack(const Words<T, N>& q, float (&v)[N]) {
     }
   }
 }
+// Two values rounded to nearest in a word, the first in the lower half.
+template <class T> __device__ __forceinline__ uint32_t round2(float lo, float hi) {
+  uint32_t r;
+  if constexpr (std::is_same<T, __half>::value) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
 template <class T, int N>
 __device__ __forceinline__ Words<T, N> pack(const float (&v)[N]) {
   uint32_t w[N * sizeof(T) / 4];
@@ -53,12 +60,8 @@ __device__ __forceinline__ Words<T, N> pack(const float (&v)[N]) {
   for (int i = 0; i < N * (int)sizeof(T) / 4; ++i) {
     if constexpr (sizeof(T) == 4) {
       w[i] = __float_as_uint(v[i]);
-    } else if constexpr (std::is_same<T, __half>::value) {
-      const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
-      w[i] = (uint32_t)__half_as_ushort(__low2half(h)) | (uint32_t)__half_as_ushort(__high2half(h)) << 16;
     } else {
-      const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-      w[i] = (uint32_t)__bfloat16_as_ushort(__low2bfloat16(h)) | (uint32_t)__bfloat16_as_ushort(__high2bfloat16(h)) << 16;
+      w[i] = round2<T>(v[2 * i], v[2 * i + 1]);
     }
   }
   return join_words(w);
@@ -155,20 +158,14 @@ __device__ __forceinline__ uint64_t drop_at(const Drop& d, uint64_t row, uint32_
   return d.key + kGamma * (d.counter + row * ((cols + 3) / 4) + col / 4 + 1);
 }
 
-// x as three bf16 values whose sum is x to 24 bits: the upper 8 bits cut off, so that they cannot overflow, the rest to nearest.
-// An x that is infinite or no number is all in the first.
-__device__ __forceinline__ void three_parts(float x, uint16_t& h, uint16_t& m, uint16_t& l) {
-  const uint32_t u = __float_as_uint(x);
-  if ((u & 0x7F800000u) == 0x7F800000u) {
-    h = (uint16_t)((u & 0x007FFFFFu) ? 0x7FFFu : u >> 16);
-    m = l = 0;
-    return;
-  }
-  h = (uint16_t)(u >> 16);
-  const float r = x - __uint_as_float(u & 0xFFFF0000u);
-  const __nv_bfloat16 rm = __float2bfloat16_rn(r);
-  m = __bfloat16_as_ushort(rm);
-  l = __bfloat16_as_ushort(__float2bfloat16_rn(r - __bfloat162float(rm)));
+// Two values as three bf16 values each whose sum is the value to 24 bits: the upper 8 bits cut off, so that they cannot overflow, the rest to
+// nearest.  Words of two, the first in the lower half.  An infinity or a NaN gives parts that are NaN.
+__device__ __forceinline__ void three_parts(float x0, float x1, uint32_t& h, uint32_t& m, uint32_t& l) {
+  const uint32_t u0 = __float_as_uint(x0), u1 = __float_as_uint(x1);
+  h = __byte_perm(u0, u1, 0x7632);
+  const float r0 = x0 - __uint_as_float(u0 & 0xFFFF0000u), r1 = x1 - __uint_as_float(u1 & 0xFFFF0000u);
+  m = round2<__nv_bfloat16>(r0, r1);
+  l = round2<__nv_bfloat16>(r0 - __uint_as_float(m << 16), r1 - __uint_as_float(m & 0xFFFF0000u));
 }
 
 // N neighbouring values (a multiple of four) in three parts to planes `plane` elements apart.
@@ -176,12 +173,12 @@ template <int N>
 __device__ __forceinline__ void store_parts(uint16_t* to, size_t plane, const float (&v)[N]) {
 #pragma unroll
   for (int g = 0; g < N; g += 4) {
-    uint16_t h[4], m[4], l[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) three_parts(v[g + i], h[i], m[i], l[i]);
-    *reinterpret_cast<uint2*>(to + g) = make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
-    *reinterpret_cast<uint2*>(to + plane + g) = make_uint2(m[0] | (uint32_t)m[1] << 16, m[2] | (uint32_t)m[3] << 16);
-    *reinterpret_cast<uint2*>(to + 2 * plane + g) = make_uint2(l[0] | (uint32_t)l[1] << 16, l[2] | (uint32_t)l[3] << 16);
+    uint2 h, m, l;
+    three_parts(v[g], v[g + 1], h.x, m.x, l.x);
+    three_parts(v[g + 2], v[g + 3], h.y, m.y, l.y);
+    *reinterpret_cast<uint2*>(to + g) = h;
+    *reinterpret_cast<uint2*>(to + plane + g) = m;
+    *reinterpret_cast<uint2*>(to + 2 * plane + g) = l;
   }
 }
 

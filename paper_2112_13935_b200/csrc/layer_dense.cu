@@ -51,58 +51,66 @@ bool four_wide(const void* p, size_t ld, uint32_t dtype) { return !p || ((uintpt
 
 size_t round_up(size_t v, size_t to) { return (v + to - 1) / to * to; }
 
-// An operand of a tensor-core product: the caller's rows where TMA takes them as they are (16-bit elements, whole 16 bytes between
-// rows and in front), otherwise a copy in the workspace.
-struct Copy { bool needed; size_t at, ld, plane, bytes; };
-Copy plan_copy(const aet_dense_desc& d, size_t rows, size_t cols, size_t ld, size_t& at) {
+// An operand of a tensor-core product: the caller's rows where TMA takes them as they are (whole 16 bytes between rows and in front), otherwise
+// a copy in the workspace; `parts`: always one, of fp32 in its three parts.
+struct Copy { bool needed; size_t at, ld, plane; };
+Copy plan_copy(const aet_dense_desc& d, size_t rows, size_t cols, size_t ld, bool parts, size_t& at) {
+  const size_t b = type_bytes(d.dtype), whole = 16 / b;
   Copy c{};
-  c.needed = d.dtype == AET_F32 || ld % 8 || (d.flags & AET_DENSE_ANY_ADDRESS);
-  c.ld = c.needed ? round_up(cols, 8) : ld;
-  c.plane = rows * c.ld;
-  c.bytes = c.needed ? round_up(c.plane * 2 * (d.dtype == AET_F32 ? 3 : 1), 256) : 0;
+  c.needed = parts || ld % whole || (d.flags & AET_DENSE_ANY_ADDRESS);
+  c.ld = !c.needed ? ld : parts ? round_up(cols, 8) : round_up(cols, whole);
+  c.plane = parts ? rows * c.ld : 0;
   c.at = at;
-  at += c.bytes;
+  if (c.needed) at += round_up(rows * c.ld * (parts ? 6 : b), 256);
   return c;
 }
-uint32_t planes_of(const aet_dense_desc& d) { return d.dtype == AET_F32 ? 3 : 1; }
+bool by_parts(const aet_dense_desc& d) { return d.dtype == AET_F32; }
 MmaOperand operand(const Copy& c, const void* src, char* ws, bool mn) { return MmaOperand{c.needed ? ws + c.at : src, c.ld, c.plane, mn}; }
-cudaError_t make_copy(const Copy& c, const aet_dense_desc& d, const void* src, size_t ld, size_t rows, size_t cols, char* ws, cudaStream_t s) {
-  if (!c.needed) return cudaSuccess;
-  return launch_planes(d.dtype, src, ld, ws + c.at, c.ld, c.plane, (uint32_t)rows, (uint32_t)cols, s);
-}
+// What there is to copy, collected so that one launch does it.
+struct Copies {
+  RowsCopy list[2];
+  int n = 0;
+  void add(const Copy& c, const aet_dense_desc& d, const void* src, size_t ld, size_t rows, size_t cols, char* ws) {
+    if (c.needed) list[n++] = RowsCopy{src, ws + c.at, ld, c.ld, c.plane, (uint32_t)rows, (uint32_t)cols, d.dtype};
+  }
+};
 
 // What a forward call does and where it keeps what it needs.
-struct Forward { bool few; MmaShape shape; Copy x, w; size_t partial, total; };
+struct Forward { bool few, mma; MmaShape shape; Copy x, w; size_t partial, total; };
 Forward plan_forward(const Dense& L, size_t rows) {
   const aet_dense_desc& d = L.d;
   Forward f{};
   f.few = rows_kernel_takes((uint32_t)rows, d.n_in);
   if (f.few) return f;
-  f.shape = mma_shape(planes_of(d), (uint32_t)rows, d.n_out, d.n_in);
-  if (!f.shape.use) return f;
-  f.x = plan_copy(d, rows, d.n_in, d.ld_x, f.total);
-  f.w = plan_copy(d, d.n_in, d.n_out, d.ld_w, f.total);
+  f.mma = mma_takes((uint32_t)rows, d.n_out, d.n_in);
+  if (!f.mma) return f;
+  f.shape = mma_shape(d.dtype, (uint32_t)rows, d.n_out, d.n_in);
+  f.x = plan_copy(d, rows, d.n_in, d.ld_x, false, f.total);
+  f.w = plan_copy(d, d.n_in, d.n_out, d.ld_w, by_parts(d), f.total);
   f.partial = f.total;
   f.total += round_up(mma_partial_floats(f.shape, (uint32_t)rows, d.n_out) * sizeof(float), 256);
   return f;
 }
 
-// ... a backward call.  dz: what the products take in dy's place, of the element type or, for the tensor cores' fp32 products, in parts.
-struct Backward { MmaShape dx, dw; Copy dz, x, w; size_t slabs, partial, total; bool as_is; };
+// ... a backward call.  dz: what the products take in dy's place, of the operands' type (dy itself where it is that); parts: the same in
+// parts, as the fp32 product for dW takes it.
+struct Backward { bool mma; MmaShape dx, dw; Copy dz, parts, x, w; size_t slabs, partial, total; };
 Backward plan_backward(const Dense& L, size_t rows) {
   const aet_dense_desc& d = L.d;
   Backward f{};
-  f.as_is = d.act == AET_ACT_NONE && !L.drop.q && !L.wide;
-  f.dx = mma_shape(planes_of(d), (uint32_t)rows, d.n_in, d.n_out);
-  f.dw = mma_shape(planes_of(d), d.n_in, d.n_out, (uint32_t)rows);
-  if (f.dx.use) {
-    f.x = plan_copy(d, rows, d.n_in, d.ld_x, f.total);
-    f.w = plan_copy(d, d.n_in, d.n_out, d.ld_w, f.total);
+  f.mma = mma_takes((uint32_t)rows, d.n_in, d.n_out) || mma_takes(d.n_in, d.n_out, (uint32_t)rows);   // (dz is laid out for one or the other)
+  if (f.mma) {
+    f.dx = mma_shape(d.dtype, (uint32_t)rows, d.n_in, d.n_out);
+    f.dw = mma_shape(d.dtype, d.n_in, d.n_out, (uint32_t)rows);
+    f.x = plan_copy(d, rows, d.n_in, d.ld_x, false, f.total);
+    f.w = plan_copy(d, d.n_in, d.n_out, d.ld_w, by_parts(d), f.total);
+    if (by_parts(d)) f.parts = plan_copy(d, rows, d.n_out, d.ld_dy, true, f.total);
   }
-  f.dz = Copy{true, f.total, round_up(d.n_out, 8), 0, 0};
-  if (f.as_is && (!f.dx.use || (d.dtype != AET_F32 && d.ld_dy % 8 == 0 && !(d.flags & AET_DENSE_ANY_ADDRESS)))) f.dz = Copy{false, 0, d.ld_dy, 0, 0};
-  f.dz.plane = rows * f.dz.ld;
-  if (f.dz.needed) f.total += round_up(f.dz.plane * (d.dtype != AET_F32 ? 2 : f.dx.use ? 6 : 4), 256);
+  f.dz = Copy{false, 0, d.ld_dy, 0};
+  if (d.act != AET_ACT_NONE || L.drop.q || L.wide || (f.mma && (d.ld_dy % (16 / type_bytes(d.dtype)) || (d.flags & AET_DENSE_ANY_ADDRESS)))) {
+    f.dz = Copy{true, f.total, round_up(d.n_out, 8), 0};
+    f.total += round_up(rows * f.dz.ld * type_bytes(d.dtype), 256);
+  }
   f.slabs = f.total;
   f.total += round_up(slope_partial_floats((uint32_t)rows, d.n_out) * sizeof(float), 256);
   f.partial = f.total;
@@ -145,13 +153,13 @@ cudaError_t dense_forward(const Dense& L, size_t rows, const void* x, const void
   p.e.vec = four_wide(y, d.ld_y, out) && four_wide(pre, d.ld_pre, out) && four_wide(residual, d.ld_residual, out);
   p.e.drop = L.drop;
   if (f.few) return launch_product_rows(p, s);
-  if (!f.shape.use) return launch_product_fma(p, s);
+  if (!f.mma) return launch_product_fma(p, s);
   char* ws = static_cast<char*>(workspace);
-  cudaError_t e = make_copy(f.x, d, x, d.ld_x, rows, d.n_in, ws, s);
-  if (e == cudaSuccess) e = make_copy(f.w, d, w, d.ld_w, d.n_in, d.n_out, ws, s);
-  if (e != cudaSuccess) return e;
-  return launch_product_mma(MmaProduct{p, operand(f.x, x, ws, false), operand(f.w, w, ws, true), d.dtype == AET_F16 ? kF16 : kBf16, planes_of(d),
-                                            f.shape, reinterpret_cast<float*>(ws + f.partial)}, s);
+  Copies copies;
+  copies.add(f.x, d, x, d.ld_x, rows, d.n_in, ws);
+  copies.add(f.w, d, w, d.ld_w, d.n_in, d.n_out, ws);
+  if (const cudaError_t e = launch_rows_copies(copies.list, copies.n, s)) return e;
+  return launch_product_mma(MmaProduct{p, operand(f.x, x, ws, false), operand(f.w, w, ws, true), d.dtype, f.shape, reinterpret_cast<float*>(ws + f.partial)}, s);
 }
 
 cudaError_t dense_backward(const Dense& L, size_t rows, const void* x, const void* w, const void* pre, const void* dy, void* dx, void* dw, void* db,
@@ -160,14 +168,15 @@ cudaError_t dense_backward(const Dense& L, size_t rows, const void* x, const voi
   const uint32_t out = L.wide ? kF32 : d.dtype;
   const Backward f = plan_backward(L, rows);
   char* ws = static_cast<char*>(workspace);
-  const bool accumulate = d.flags & AET_DENSE_ACCUMULATE, products = dx || dw;
+  const bool accumulate = d.flags & AET_DENSE_ACCUMULATE;
 
-  if (db || (products && f.dz.needed)) {
+  const bool want_dz = f.dz.needed && (dx || (dw && !f.parts.needed)), want_parts = f.parts.needed && dw;
+  if (db || want_dz || want_parts) {
     SlopeLaunch p{};
     p.dy = dy; p.ld_dy = d.ld_dy;
     p.pre = d.act == AET_ACT_NONE ? nullptr : pre; p.ld_pre = d.ld_pre;
-    p.dz = products && f.dz.needed ? ws + f.dz.at : nullptr; p.ld_dz = f.dz.ld;
-    p.plane = d.dtype == AET_F32 && f.dx.use ? f.dz.plane : 0;
+    p.dz = want_dz ? ws + f.dz.at : nullptr; p.ld_dz = f.dz.ld;
+    if (want_parts) p.parts = reinterpret_cast<uint16_t*>(ws + f.parts.at), p.ld_parts = f.parts.ld, p.plane = f.parts.plane;
     p.db = db; p.db_type = out; p.accumulate = accumulate;
     p.type = out; p.act = d.act; p.dz_bf16 = L.wide;
     p.rows = (uint32_t)rows; p.cols = d.n_out;
@@ -176,8 +185,13 @@ cudaError_t dense_backward(const Dense& L, size_t rows, const void* x, const voi
     if (const cudaError_t e = launch_slope(p, s)) return e;
   }
   const void* dz = f.dz.needed ? ws + f.dz.at : dy;
-  const uint32_t type16 = d.dtype == AET_F16 ? kF16 : kBf16;
   float* partial = reinterpret_cast<float*>(ws + f.partial);
+  if (f.mma) {
+    Copies copies;
+    if (dx) copies.add(f.w, d, w, d.ld_w, d.n_in, d.n_out, ws);
+    if (dw) copies.add(f.x, d, x, d.ld_x, rows, d.n_in, ws);
+    if (const cudaError_t e = launch_rows_copies(copies.list, copies.n, s)) return e;
+  }
   if (dx) {
     Product p{};
     p.a = dz; p.a_row = f.dz.ld; p.a_col = 1;
@@ -185,14 +199,8 @@ cudaError_t dense_backward(const Dense& L, size_t rows, const void* x, const voi
     p.type = d.dtype;
     p.m = (uint32_t)rows; p.n = d.n_in; p.k = d.n_out;
     p.e = plain_epilogue(dx, d.ld_dx, out, false);
-    cudaError_t e;
-    if (!f.dx.use) {
-      e = launch_product_fma(p, s);
-    } else {
-      e = make_copy(f.w, d, w, d.ld_w, d.n_in, d.n_out, ws, s);
-      if (e == cudaSuccess)
-        e = launch_product_mma(MmaProduct{p, operand(f.dz, dy, ws, false), operand(f.w, w, ws, false), type16, planes_of(d), f.dx, partial}, s);
-    }
+    const cudaError_t e = f.mma ? launch_product_mma(MmaProduct{p, operand(f.dz, dy, ws, false), operand(f.w, w, ws, false), d.dtype, f.dx, partial}, s)
+                                : launch_product_fma(p, s);
     if (e != cudaSuccess) return e;
   }
   if (dw) {
@@ -202,14 +210,8 @@ cudaError_t dense_backward(const Dense& L, size_t rows, const void* x, const voi
     p.type = d.dtype;
     p.m = d.n_in; p.n = d.n_out; p.k = (uint32_t)rows;
     p.e = plain_epilogue(dw, d.ld_dw, out, accumulate);
-    cudaError_t e;
-    if (!f.dw.use) {
-      e = launch_product_fma(p, s);
-    } else {
-      e = make_copy(f.x, d, x, d.ld_x, rows, d.n_in, ws, s);
-      if (e == cudaSuccess)
-        e = launch_product_mma(MmaProduct{p, operand(f.x, x, ws, true), operand(f.dz, dy, ws, true), type16, planes_of(d), f.dw, partial}, s);
-    }
+    const MmaOperand b = f.parts.needed ? operand(f.parts, nullptr, ws, true) : operand(f.dz, dy, ws, true);
+    const cudaError_t e = f.mma ? launch_product_mma(MmaProduct{p, operand(f.x, x, ws, true), b, d.dtype, f.dw, partial}, s) : launch_product_fma(p, s);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;

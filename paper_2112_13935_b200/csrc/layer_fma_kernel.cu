@@ -96,11 +96,17 @@ __global__ void __launch_bounds__(kThreads) product_fma_kernel(const Product p, 
 
 }  // namespace
 
+// as many CTAs along k as there are SMs for them, each with 32 and more of it
+uint32_t fma_split(uint32_t m, uint32_t n, uint32_t k) {
+  const uint64_t tiles = ((uint64_t)n + kTile - 1) / kTile * (((uint64_t)m + kTile - 1) / kTile);
+  uint32_t split = 1;
+  while (split < 8 && tiles * split * 2 <= 148 && k >= 32 * 2 * split) split *= 2;
+  return split;
+}
+
 cudaError_t launch_product_fma(const Product& p, cudaStream_t s) {
   const uint64_t tiles_n = (p.n + kTile - 1) / kTile, tiles = tiles_n * ((p.m + kTile - 1) / kTile);
-  // as many CTAs along k as there are SMs for them, each with 32 and more of it
-  uint32_t split = 1;
-  while (split < 8 && tiles * split * 2 <= 148 && p.k >= 32 * 2 * split) split *= 2;
+  const uint32_t split = fma_split(p.m, p.n, p.k);
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(tiles * split));
   cfg.blockDim = dim3(kThreads);

@@ -43,42 +43,53 @@ struct Product {
 
 // Small products: 64 x 64 tiles on FMAs, k split over the CTAs of a cluster.
 cudaError_t launch_product_fma(const Product& p, cudaStream_t s);
+uint32_t fma_split(uint32_t m, uint32_t n, uint32_t k);    // CTAs along k
 
 // Up to eight rows of A along k against a B across it (see layer_rows_kernel.cu).
 bool rows_kernel_takes(uint32_t m, uint32_t k);
 cudaError_t launch_product_rows(const Product& p, cudaStream_t s);
 
-// Large products (see layer_mma_kernel.cu).  An operand of a tensor-core product: 16-bit elements, rows `ld` elements apart and from
-// 16-byte boundaries on, `planes` of them `plane` elements apart (three: the parts of fp32); mn: its rows run along k, not across.
+// Large products (see layer_mma_kernel.cu and, for fp32, layer_f32_kernel.cu).  An operand of a tensor-core product: rows `ld` elements
+// apart and from 16-byte boundaries on; mn: its rows run along k, not across.  fp32: A as it is, B as its three bf16 parts, `plane`
+// elements apart.
 struct MmaOperand {
   const void* p;
   size_t ld, plane;
   uint32_t mn;
 };
 struct MmaShape {
-  uint32_t use;      // whether the tensor cores take the product at all
   uint32_t pair;     // two CTAs share a tile
   uint32_t splits;   // parts k is split into
 };
 struct MmaProduct {
   Product p;         // m, n, k and the epilogue; a and b stand here:
   MmaOperand a, b;
-  uint32_t type, planes;   // kBf16 or kF16; 1, or 3 (then kBf16)
+  uint32_t type;
   MmaShape shape;
   float* partial;    // mma_partial_floats() of workspace
 };
-MmaShape mma_shape(uint32_t planes, uint32_t m, uint32_t n, uint32_t k);
+bool mma_takes(uint32_t m, uint32_t n, uint32_t k);   // rather than the FMA kernel
+MmaShape mma_shape(uint32_t type, uint32_t m, uint32_t n, uint32_t k);
 size_t mma_partial_floats(const MmaShape& s, uint32_t m, uint32_t n);
 cudaError_t launch_product_mma(const MmaProduct& m, cudaStream_t s);
-// Rows onto a stride that TMA takes (ld_dst a multiple of 8): 16-bit elements as they are, fp32 as three bf16 planes.
-cudaError_t launch_planes(uint32_t type, const void* src, size_t ld, void* dst, size_t ld_dst, size_t plane, uint32_t rows, uint32_t cols, cudaStream_t s);
+cudaError_t launch_product_f32(const MmaProduct& m, cudaStream_t s);
+// Rows onto a stride that TMA takes, whole 16 bytes and from a 16-byte boundary: as they are, or (plane non-zero) fp32 as three bf16 parts
+// `plane` elements apart.  Up to two arrays in one launch.
+struct RowsCopy {
+  const void* src;
+  void* dst;
+  size_t ld, ld_dst, plane;
+  uint32_t rows, cols, type;
+};
+cudaError_t launch_rows_copies(const RowsCopy* copies, int n, cudaStream_t s);
 
-// dz = drop(dy) act'(pre), to `dz` (null: not kept; plane non-zero: as three bf16 parts, `plane` elements apart), and its sums over
-// the rows to db.
+// dz = drop(dy) act'(pre), to `dz` (null: not kept), to `parts` (null: not wanted) as three bf16 parts `plane` elements apart, and its sums
+// over the rows to db.
 struct SlopeLaunch {
   const void *dy, *pre;   // pre null: act is none
   void *dz, *db;          // db null: no sums
-  size_t ld_dy, ld_pre, ld_dz, plane;
+  uint16_t* parts;        // rows ld_parts apart
+  size_t ld_dy, ld_pre, ld_dz, ld_parts, plane;
   uint32_t type, db_type, act, accumulate;   // of dy and pre; accumulate: db += sums
   uint32_t dz_bf16;       // dz is bf16 where dy is fp32
   uint32_t rows, cols;

@@ -57,9 +57,8 @@ __global__ void __launch_bounds__(kThreads, 4) slope_kernel(const SlopeLaunch p,
             for (int k = 0; k < N; ++k) v[k] *= act_slope<T>(kSilu, z[k]);
           }
         }
-        if (p.dz && p.plane) {
-          store_parts<N>(static_cast<uint16_t*>(p.dz) + r * p.ld_dz + col, p.plane, v);   // (0 past the last column)
-        } else if (p.dz && p.dz_bf16) {
+        if (p.parts) store_parts<N>(p.parts + r * p.ld_parts + col, p.plane, v);   // (0 past the last column)
+        if (p.dz && p.dz_bf16) {
           store_n<__nv_bfloat16, N>(static_cast<__nv_bfloat16*>(p.dz) + r * p.ld_dz + col, whole, n, v);
         } else if (p.dz) {
           store_n<T, N>(static_cast<T*>(p.dz) + r * p.ld_dz + col, whole, n, v);
@@ -123,7 +122,7 @@ template <class T>
 cudaError_t run(const SlopeLaunch& p, cudaStream_t s) {
   constexpr int N = 16 / (int)sizeof(T);
   const uint32_t slabs = slabs_of(p.rows, p.cols);
-  const bool vec = aligned(p.dy, p.ld_dy, N, sizeof(T)) && aligned(p.pre, p.ld_pre, N, sizeof(T)) && (p.plane || aligned(p.dz, p.ld_dz, N, p.dz_bf16 ? 2 : sizeof(T)));
+  const bool vec = aligned(p.dy, p.ld_dy, N, sizeof(T)) && aligned(p.pre, p.ld_pre, N, sizeof(T)) && aligned(p.dz, p.ld_dz, N, p.dz_bf16 ? 2 : sizeof(T));
   if (vec) go<T, N, true>(p, slabs, s);
   else go<T, 4, false>(p, slabs, s);
   if (p.db) {
