@@ -278,36 +278,44 @@ def _dtype(t) -> int:
         raise AetError(1, f"element type {t} is not float32, bfloat16 or float16") from None
 
 
-def _raw_stream(t, stream):
-    """The stream given, or the current one, of the current device, which the tensors have to be on."""
-    import torch
-    dev = torch._C._cuda_getDevice() if t.is_cuda else -2     # (torch.cuda.current_device and current_stream take longer than the call)
-    if t.get_device() != dev:
+_cuda = None
+
+
+def _stream_of(dev: int, t, stream):
+    """The stream given, or the current one, of the current device, which the tensors have to be on.
+
+    torch.cuda.current_device() and current_stream() take longer than a whole call here; this is what they ask."""
+    global _cuda
+    if _cuda is None:
+        import torch
+        _cuda = torch._C
+    if dev < 0 or dev != _cuda._cuda_getDevice():
         raise AetError(1, f"tensors have to be on the current CUDA device, not on {t.device}")
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(dev)
+        return _cuda._cuda_getCurrentRawStream(dev)
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
-def _at(t, like, shape, what, ld=None):
-    """Address of a matrix (its rows `ld` elements apart) or vector of `like`'s type and device (None: null)."""
+def _at(t, dtype, dev, shape, what, ld):
+    """Address of a matrix of rows `ld` elements apart, or (ld None) of a vector (t None: null)."""
     if t is None:
         return None
-    if t.dtype is not like.dtype or t.shape != shape or t.get_device() != like.get_device():
-        raise AetError(1, f"{what}: {tuple(t.shape)} of {t.dtype} on {t.device}, expected {tuple(shape)} of {like.dtype} on {like.device}")
+    if t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.stride() == ((ld, 1) if ld else (1,)):
+        return t.data_ptr()
     s = t.stride()
-    if s != ((1,) if ld is None and len(s) == 1 else (ld, 1)) and t.numel():     # (what an index of one value strides by does not matter)
-        if (shape[-1] > 1 and s[-1] != 1) or (ld is not None and shape[0] > 1 and s[0] != ld):
-            raise AetError(1, f"{what}: strides {s}, expected rows {ld} elements apart of neighbouring elements")
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev:
+        raise AetError(1, f"{what}: {tuple(t.shape)} of {t.dtype} on {t.device}, expected {tuple(shape)} of {dtype} on CUDA device {dev}")
+    if t.numel() and ((shape[-1] > 1 and s[-1] != 1) or (ld and shape[0] > 1 and s[0] != ld)):   # (what an index of one value strides by does not matter)
+        raise AetError(1, f"{what}: strides {s}, expected rows {ld} elements apart of neighbouring elements")
     return t.data_ptr()
 
 
-def _row_major(t, like, shape, what):
+def _row_major(t, dtype, dev, shape, what):
     """Address and ld of a matrix whose rows may be any distance apart."""
     if t is None:
         return None, 0
-    ld = t.stride(0) if len(shape) == 2 and shape[0] > 1 else shape[-1]
-    return _at(t, like, shape, what, ld), ld
+    ld = t.stride(0) if shape[0] > 1 and len(t.shape) == 2 else shape[1]
+    return _at(t, dtype, dev, shape, what, ld), ld
 
 
 def aet_dropout_spec(seed: int, client: int = 0, counter: int = 0, rate: float = 0.0):
@@ -316,28 +324,28 @@ def aet_dropout_spec(seed: int, client: int = 0, counter: int = 0, rate: float =
 
 def aet_dropout(drop, x, y, residual=None, stream=None):
     """y = residual + dropout(x); see include/aet.h for which elements a (seed, client, counter) drops."""
-    shape = x.shape
+    shape, dtype, dev = x.shape, x.dtype, x.get_device()
     if len(shape) != 2:
         raise AetError(1, "x: a matrix is expected")
-    _check(None, _lib.load().aet_dropout(
-        _dtype(x.dtype), shape[0], shape[1], C.addressof(drop), *_row_major(x, x, shape, "x"), *_row_major(residual, x, shape, "residual"),
-        *_row_major(y, x, shape, "y"), _raw_stream(x, stream)))
+    px, ld_x = _row_major(x, dtype, dev, shape, "x")
+    pr, ld_r = _row_major(residual, dtype, dev, shape, "residual")
+    py, ld_y = _row_major(y, dtype, dev, shape, "y")
+    _check(None, _lib.load().aet_dropout(_dtype(dtype), shape[0], shape[1], C.addressof(drop), px, ld_x, pr, ld_r, py, ld_y, _stream_of(dev, x, stream)))
 
 
 def aet_cross_entropy(logits, labels, loss=None, dlogits=None, top=None, weight=None, scale: float = 1.0, stream=None):
     """Softmax cross-entropy of each row, its gradient times `scale` (and `weight`), and the lowest index of its maximum."""
     import torch
-    shape = logits.shape
+    shape, dtype, dev = logits.shape, logits.dtype, logits.get_device()
     if len(shape) != 2:
         raise AetError(1, "logits: a matrix is expected")
-    at = []
-    for t, kind, what in ((labels, torch.int32, "labels"), (weight, torch.float32, "weight"), (loss, torch.float32, "loss"), (top, torch.int32, "top")):
-        if t is not None and (t.dtype is not kind or t.shape != shape[:1] or not t.is_contiguous() or t.get_device() != logits.get_device()):
-            raise AetError(1, f"{what}: {tuple(t.shape)} of {t.dtype} on {t.device}, expected {shape[0]} neighbouring {kind} on {logits.device}")
-        at.append(None if t is None else t.data_ptr())
+    one = shape[:1]
+    pz, ld_z = _row_major(logits, dtype, dev, shape, "logits")
+    pg, ld_g = _row_major(dlogits, dtype, dev, shape, "dlogits")
     _check(None, _lib.load().aet_cross_entropy(
-        _dtype(logits.dtype), shape[0], shape[1], *_row_major(logits, logits, shape, "logits"), at[0], at[1], scale, at[2],
-        *_row_major(dlogits, logits, shape, "dlogits"), at[3], _raw_stream(logits, stream)))
+        _dtype(dtype), shape[0], shape[1], pz, ld_z, _at(labels, torch.int32, dev, one, "labels", None),
+        _at(weight, torch.float32, dev, one, "weight", None), scale, _at(loss, torch.float32, dev, one, "loss", None), pg, ld_g,
+        _at(top, torch.int32, dev, one, "top", None), _stream_of(dev, logits, stream)))
 
 
 def aet_dense(n_in: int, n_out: int, dtype=None, act: str = "none", dropout=None, ld_in: int = 0, ld_out: int = 0, ld_w: int = 0, flags: int = 0, **lds):
@@ -368,10 +376,10 @@ def aet_dense_workspace(d, rows: int, backward: bool = False) -> int:
     return int(n.value)
 
 
-def _space(workspace, like):
+def _space(workspace, dev):
     if workspace is None:
         return None, 0
-    if workspace.get_device() != like.get_device() or not workspace.is_contiguous():
+    if workspace.get_device() != dev or not workspace.is_contiguous():
         raise AetError(1, "workspace: a contiguous tensor on the layer's device is expected")
     return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
@@ -379,29 +387,31 @@ def _space(workspace, like):
 def _rows_of(d, x, cols, what):
     if len(x.shape) != 2 or x.shape[1] != cols or _dtype(x.dtype) != d.dtype:
         raise AetError(1, f"{what}: {tuple(x.shape)} of {x.dtype} does not fit the descriptor")
-    return x.shape[0]
+    return x.shape[0], x.dtype, x.get_device()
 
 
 def aet_dense_forward(d, x, w, bias, y, residual=None, pre=None, workspace=None, stream=None):
     """y = residual + dropout(act(x w + bias)); pre: where x w + bias goes for the backward pass."""
-    rows, n_in, n_out = _rows_of(d, x, d.n_in, "x"), d.n_in, d.n_out
+    n_in, n_out = d.n_in, d.n_out
+    rows, t, dev = _rows_of(d, x, n_in, "x")
     out = (rows, n_out)
-    ws, size = _space(workspace, x)
+    ws, size = _space(workspace, dev)
     _check(None, _lib.load().aet_dense_forward(
-        C.addressof(d), rows, _at(x, x, (rows, n_in), "x", d.ld_x), _at(w, x, (n_in, n_out), "w", d.ld_w), _at(bias, x, (n_out,), "bias"),
-        _at(residual, x, out, "residual", d.ld_residual), _at(y, x, out, "y", d.ld_y), _at(pre, x, out, "pre", d.ld_pre), ws, size,
-        _raw_stream(x, stream)))
+        C.addressof(d), rows, _at(x, t, dev, (rows, n_in), "x", d.ld_x), _at(w, t, dev, (n_in, n_out), "w", d.ld_w), _at(bias, t, dev, (n_out,), "bias", None),
+        _at(residual, t, dev, out, "residual", d.ld_residual), _at(y, t, dev, out, "y", d.ld_y), _at(pre, t, dev, out, "pre", d.ld_pre), ws, size,
+        _stream_of(dev, x, stream)))
 
 
 def aet_dense_backward(d, x, w, dy, pre=None, dx=None, dw=None, db=None, workspace=None, stream=None):
     """dx, dw and db (any of them None) of the layer from dy."""
-    rows, n_in, n_out = _rows_of(d, dy, d.n_out, "dy"), d.n_in, d.n_out
-    out = (rows, n_out)
-    ws, size = _space(workspace, dy)
+    n_in, n_out = d.n_in, d.n_out
+    rows, t, dev = _rows_of(d, dy, n_out, "dy")
+    out, into, weights = (rows, n_out), (rows, n_in), (n_in, n_out)
+    ws, size = _space(workspace, dev)
     _check(None, _lib.load().aet_dense_backward(
-        C.addressof(d), rows, _at(x, dy, (rows, n_in), "x", d.ld_x), _at(w, dy, (n_in, n_out), "w", d.ld_w), _at(pre, dy, out, "pre", d.ld_pre),
-        _at(dy, dy, out, "dy", d.ld_dy), _at(dx, dy, (rows, n_in), "dx", d.ld_dx), _at(dw, dy, (n_in, n_out), "dw", d.ld_dw),
-        _at(db, dy, (n_out,), "db"), ws, size, _raw_stream(dy, stream)))
+        C.addressof(d), rows, _at(x, t, dev, into, "x", d.ld_x), _at(w, t, dev, weights, "w", d.ld_w), _at(pre, t, dev, out, "pre", d.ld_pre),
+        _at(dy, t, dev, out, "dy", d.ld_dy), _at(dx, t, dev, into, "dx", d.ld_dx), _at(dw, t, dev, weights, "dw", d.ld_dw),
+        _at(db, t, dev, (n_out,), "db", None), ws, size, _stream_of(dev, dy, stream)))
 
 
 class Session:

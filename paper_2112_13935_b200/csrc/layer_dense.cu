@@ -92,9 +92,9 @@ Forward plan_forward(const Dense& L, size_t rows) {
   return f;
 }
 
-// ... a backward call.  dz: what the products take in dy's place, of the operands' type (dy itself where it is that); parts: the same in
-// parts, as the fp32 product for dW takes it.
-struct Backward { bool mma; MmaShape dx, dw; Copy dz, parts, x, w; size_t slabs, partial, total; };
+// ... a backward call.  dz: what the products take in dy's place, of the operands' type, as the tensor cores take it, or in fp32 (dy itself
+// where it is that); parts: the same in parts, as the fp32 product for dW takes it.
+struct Backward { bool mma; MmaShape dx, dw; Copy dz, parts, x, w; uint32_t dz_type; size_t slabs, partial, total; };
 Backward plan_backward(const Dense& L, size_t rows) {
   const aet_dense_desc& d = L.d;
   Backward f{};
@@ -109,7 +109,8 @@ Backward plan_backward(const Dense& L, size_t rows) {
   f.dz = Copy{false, 0, d.ld_dy, 0};
   if (d.act != AET_ACT_NONE || L.drop.q || L.wide || (f.mma && (d.ld_dy % (16 / type_bytes(d.dtype)) || (d.flags & AET_DENSE_ANY_ADDRESS)))) {
     f.dz = Copy{true, f.total, round_up(d.n_out, 8), 0};
-    f.total += round_up(rows * f.dz.ld * type_bytes(d.dtype), 256);
+    f.dz_type = f.mma || L.wide ? d.dtype : kF32;
+    f.total += round_up(rows * f.dz.ld * type_bytes(f.dz_type), 256);
   }
   f.slabs = f.total;
   f.total += round_up(slope_partial_floats((uint32_t)rows, d.n_out) * sizeof(float), 256);
@@ -178,13 +179,14 @@ cudaError_t dense_backward(const Dense& L, size_t rows, const void* x, const voi
     p.dz = want_dz ? ws + f.dz.at : nullptr; p.ld_dz = f.dz.ld;
     if (want_parts) p.parts = reinterpret_cast<uint16_t*>(ws + f.parts.at), p.ld_parts = f.parts.ld, p.plane = f.parts.plane;
     p.db = db; p.db_type = out; p.accumulate = accumulate;
-    p.type = out; p.act = d.act; p.dz_bf16 = L.wide;
+    p.type = out; p.act = d.act; p.dz_type = f.dz_type;
     p.rows = (uint32_t)rows; p.cols = d.n_out;
     p.drop = L.drop;
     p.partial = reinterpret_cast<float*>(ws + f.slabs);
     if (const cudaError_t e = launch_slope(p, s)) return e;
   }
   const void* dz = f.dz.needed ? ws + f.dz.at : dy;
+  const bool dz_f32 = f.dz.needed && f.dz_type == kF32 && d.dtype != AET_F32;
   float* partial = reinterpret_cast<float*>(ws + f.partial);
   if (f.mma) {
     Copies copies;
@@ -196,7 +198,7 @@ cudaError_t dense_backward(const Dense& L, size_t rows, const void* x, const voi
     Product p{};
     p.a = dz; p.a_row = f.dz.ld; p.a_col = 1;
     p.b = w; p.b_row = 1; p.b_col = d.ld_w;
-    p.type = d.dtype;
+    p.type = d.dtype; p.a_f32 = dz_f32;
     p.m = (uint32_t)rows; p.n = d.n_in; p.k = d.n_out;
     p.e = plain_epilogue(dx, d.ld_dx, out, false);
     const cudaError_t e = f.mma ? launch_product_mma(MmaProduct{p, operand(f.dz, dy, ws, false), operand(f.w, w, ws, false), d.dtype, f.dx, partial}, s)
@@ -207,7 +209,7 @@ cudaError_t dense_backward(const Dense& L, size_t rows, const void* x, const voi
     Product p{};
     p.a = x; p.a_row = 1; p.a_col = d.ld_x;
     p.b = dz; p.b_row = f.dz.ld; p.b_col = 1;
-    p.type = d.dtype;
+    p.type = d.dtype; p.b_f32 = dz_f32;
     p.m = d.n_in; p.n = d.n_out; p.k = (uint32_t)rows;
     p.e = plain_epilogue(dw, d.ld_dw, out, accumulate);
     const MmaOperand b = f.parts.needed ? operand(f.parts, nullptr, ws, true) : operand(f.dz, dy, ws, true);

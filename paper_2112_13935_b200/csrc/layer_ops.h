@@ -39,9 +39,10 @@ struct Product {
   uint32_t type;
   uint32_t m, n, k;
   Epilogue e;
+  uint32_t a_f32, b_f32;     // that operand is fp32 beside a 16-bit `type` (launch_product_fma only)
 };
 
-// Small products: 64 x 64 tiles on FMAs, k split over the CTAs of a cluster.
+// Small products, on FMAs (see layer_fma_kernel.cu).
 cudaError_t launch_product_fma(const Product& p, cudaStream_t s);
 uint32_t fma_split(uint32_t m, uint32_t n, uint32_t k);    // CTAs along k
 
@@ -91,7 +92,7 @@ struct SlopeLaunch {
   uint16_t* parts;        // rows ld_parts apart
   size_t ld_dy, ld_pre, ld_dz, ld_parts, plane;
   uint32_t type, db_type, act, accumulate;   // of dy and pre; accumulate: db += sums
-  uint32_t dz_bf16;       // dz is bf16 where dy is fp32
+  uint32_t dz_type;       // dy's, bf16 where dy is fp32, or fp32
   uint32_t rows, cols;
   Drop drop;
   float* partial;         // slope_partial_floats() of workspace

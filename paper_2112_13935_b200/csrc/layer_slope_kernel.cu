@@ -13,6 +13,15 @@ namespace {
 
 constexpr int kThreads = 256, kRows = 2;
 
+template <int N>
+__device__ __forceinline__ void store_wide(float* p, bool whole, int n, const float (&v)[N]) {
+#pragma unroll
+  for (int g = 0; g < N; g += 4) {
+    const float q[4] = {v[g], v[g + 1], v[g + 2], v[g + 3]};
+    store_n<float, 4>(p + g, whole, n - g, q);
+  }
+}
+
 template <class T, int N, bool kVec>
 __global__ void __launch_bounds__(kThreads, 4) slope_kernel(const SlopeLaunch p, const uint32_t slabs, const uint32_t log) {
   __shared__ __align__(16) float sums[kThreads * N];
@@ -58,11 +67,9 @@ __global__ void __launch_bounds__(kThreads, 4) slope_kernel(const SlopeLaunch p,
           }
         }
         if (p.parts) store_parts<N>(p.parts + r * p.ld_parts + col, p.plane, v);   // (0 past the last column)
-        if (p.dz && p.dz_bf16) {
-          store_n<__nv_bfloat16, N>(static_cast<__nv_bfloat16*>(p.dz) + r * p.ld_dz + col, whole, n, v);
-        } else if (p.dz) {
-          store_n<T, N>(static_cast<T*>(p.dz) + r * p.ld_dz + col, whole, n, v);
-        }
+        if (p.dz && p.dz_type == kF32) store_wide<N>(static_cast<float*>(p.dz) + r * p.ld_dz + col, whole, n, v);
+        else if (p.dz && sizeof(T) == 4) store_n<__nv_bfloat16, N>(static_cast<__nv_bfloat16*>(p.dz) + r * p.ld_dz + col, whole, n, v);
+        else if (p.dz) store_n<T, N>(static_cast<T*>(p.dz) + r * p.ld_dz + col, whole, n, v);
 #pragma unroll
         for (int k = 0; k < N; ++k) acc[k] += v[k];
       }
@@ -122,7 +129,7 @@ template <class T>
 cudaError_t run(const SlopeLaunch& p, cudaStream_t s) {
   constexpr int N = 16 / (int)sizeof(T);
   const uint32_t slabs = slabs_of(p.rows, p.cols);
-  const bool vec = aligned(p.dy, p.ld_dy, N, sizeof(T)) && aligned(p.pre, p.ld_pre, N, sizeof(T)) && aligned(p.dz, p.ld_dz, N, p.dz_bf16 ? 2 : sizeof(T));
+  const bool vec = aligned(p.dy, p.ld_dy, N, sizeof(T)) && aligned(p.pre, p.ld_pre, N, sizeof(T)) && aligned(p.dz, p.ld_dz, N, type_bytes(p.dz_type));
   if (vec) go<T, N, true>(p, slabs, s);
   else go<T, 4, false>(p, slabs, s);
   if (p.db) {
