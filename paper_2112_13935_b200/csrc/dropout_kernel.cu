@@ -16,6 +16,7 @@ constexpr int kThreads = 256, kRows = 3;
 template <class T, int N, bool kVec>
 __global__ void __launch_bounds__(kThreads, 3) dropout_kernel(const size_t rows, const uint32_t cols, const Drop d, const T* x, const size_t ld_x, const T* res,
                                                            const size_t ld_res, T* y, const size_t ld_y, const uint32_t log) {
+  in_line();
   const uint32_t col = ((blockIdx.x << log) + (threadIdx.x & ((1u << log) - 1))) * N;
   if (col >= cols) return;
   const int n = (int)min((uint32_t)N, cols - col);
@@ -56,9 +57,8 @@ cudaError_t go(size_t rows, uint32_t cols, const Drop& d, const void* x, size_t 
   const uint64_t across = (((uint64_t)cols + N - 1) / N + (1u << log) - 1) >> log;     // CTAs across the columns
   // eight CTAs for each of 148 SMs, which go round the rows
   const uint64_t at_once = (uint64_t)(kThreads >> log) * kRows, most = (rows + at_once - 1) / at_once, want = (148 * 8 + across - 1) / across;
-  dropout_kernel<T, N, kVec><<<dim3((unsigned)across, (unsigned)(most < want ? most : want)), kThreads, 0, s>>>(
-      rows, cols, d, (const T*)x, ld_x, (const T*)res, ld_res, (T*)y, ld_y, log);
-  return cudaGetLastError();
+  return launch(dropout_kernel<T, N, kVec>, dim3((unsigned)across, (unsigned)(most < want ? most : want)), kThreads, 0, 1, s, rows, cols, d, (const T*)x,
+                ld_x, (const T*)res, ld_res, (T*)y, ld_y, log);
 }
 template <class T>
 cudaError_t run(size_t rows, uint32_t cols, const Drop& d, const void* x, size_t ld_x, const void* res, size_t ld_res, void* y, size_t ld_y,

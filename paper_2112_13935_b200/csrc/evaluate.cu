@@ -4,6 +4,7 @@
 
 #include "aet_kernels.h"
 #include "evaluate.h"
+#include "layer_launch.h"
 
 namespace aet {
 using namespace layer;
@@ -88,6 +89,7 @@ __device__ __forceinline__ double cta_sum(double v, double* part) {   // over th
 }
 __global__ void __launch_bounds__(kThreads) tally_kernel(const float* loss, const int32_t* top, const int32_t* y, uint32_t rows, uint32_t classes, Tally* t) {
   __shared__ double part[kThreads / 32];
+  in_line();
   double sum = 0., right = 0., bad = 0.;     // (counts below 2^53)
   for (uint32_t i = threadIdx.x; i < rows; i += kThreads) {
     const bool known = (uint32_t)y[i] < classes;
@@ -106,6 +108,7 @@ __global__ void __launch_bounds__(kThreads) tally_kernel(const float* loss, cons
 }
 __global__ void __launch_bounds__(kThreads) l2_kernel(const float* w, float* g, size_t count, float lambda, double n, Tally* t) {
   __shared__ double part[kThreads / 32];
+  in_line();
   double sum = 0.;
 #pragma unroll 8
   for (size_t i = threadIdx.x; i < count; i += kThreads) {
@@ -167,8 +170,7 @@ cudaError_t eval_rows(const EvalModel& m, const float* w, const float* x, const 
   p.type = kF32; p.classes = classes;
   p.scale = (float)(1.0 / (double)n);
   AET_STEP(launch_loss(p, s));
-  tally_kernel<<<1, kThreads, 0, s>>>(p.loss, p.top, y, (uint32_t)rows, classes, tally);
-  AET_STEP(cudaGetLastError());
+  AET_STEP(launch(tally_kernel, dim3(1), kThreads, 0, 1, s, p.loss, p.top, y, (uint32_t)rows, classes, tally));
   if (!back) return cudaSuccess;
   const float* dy = f32(sp.dlogits);
   for (uint32_t l = L; l-- > 0;) {
@@ -185,10 +187,10 @@ cudaError_t eval_l2(const EvalModel& m, const float* w, size_t n, Tally* tally, 
   size_t off = 0;
   for (uint32_t l = 0; l < m.n_layers; ++l) {
     const size_t count = (size_t)m.dims[l] * m.dims[l + 1];
-    l2_kernel<<<1, kThreads, 0, s>>>(w + off, gradient ? gradient + off : nullptr, count, m.l2, (double)n, tally);
+    if (const cudaError_t e = launch(l2_kernel, dim3(1), kThreads, 0, 1, s, w + off, gradient ? gradient + off : nullptr, count, m.l2, (double)n, tally)) return e;
     off += count + m.dims[l + 1];
   }
-  return cudaGetLastError();
+  return cudaSuccess;
 }
 
 }  // namespace aet

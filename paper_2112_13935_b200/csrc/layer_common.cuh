@@ -6,6 +6,7 @@
 #include <type_traits>
 
 #include "aet_rng.h"
+#include "layer_launch.h"
 #include "layer_ops.h"
 
 namespace aet {

@@ -30,6 +30,7 @@ __device__ __forceinline__ void take8(const T* s, int n, uint32_t (&w)[8 * sizeo
 }
 
 __global__ void __launch_bounds__(kThreads) rows_copy_kernel(const Jobs jobs) {
+  in_line();
   const int which = blockIdx.x >= jobs.first;
   const RowsCopy& j = jobs.job[which];
   const uint32_t log = jobs.log[which], cta = blockIdx.x - (which ? jobs.first : 0);
@@ -76,8 +77,7 @@ cudaError_t launch_rows_copies(const RowsCopy* copies, int n, cudaStream_t s) {
     ctas += (copies[i].rows + at_once - 1) / at_once * jobs.across[i];
     if (i == 0) jobs.first = (uint32_t)ctas;
   }
-  rows_copy_kernel<<<(unsigned)ctas, kThreads, 0, s>>>(jobs);
-  return cudaGetLastError();
+  return launch(rows_copy_kernel, dim3((unsigned)ctas), kThreads, 0, 1, s, jobs);
 }
 
 }  // namespace layer

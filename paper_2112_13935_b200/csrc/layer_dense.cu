@@ -82,7 +82,7 @@ Forward plan_forward(const Dense& L, size_t rows) {
   Forward f{};
   f.few = rows_kernel_takes((uint32_t)rows, d.n_in);
   if (f.few) return f;
-  f.mma = mma_takes((uint32_t)rows, d.n_out, d.n_in);
+  f.mma = mma_takes(d.dtype, (uint32_t)rows, d.n_out, d.n_in);
   if (!f.mma) return f;
   f.shape = mma_shape(d.dtype, (uint32_t)rows, d.n_out, d.n_in);
   f.x = plan_copy(d, rows, d.n_in, d.ld_x, false, f.total);
@@ -98,7 +98,7 @@ struct Backward { bool mma; MmaShape dx, dw; Copy dz, parts, x, w; uint32_t dz_t
 Backward plan_backward(const Dense& L, size_t rows) {
   const aet_dense_desc& d = L.d;
   Backward f{};
-  f.mma = mma_takes((uint32_t)rows, d.n_in, d.n_out) || mma_takes(d.n_in, d.n_out, (uint32_t)rows);   // (dz is laid out for one or the other)
+  f.mma = mma_takes(d.dtype, (uint32_t)rows, d.n_in, d.n_out) || mma_takes(d.dtype, d.n_in, d.n_out, (uint32_t)rows);   // (dz is laid out for one or the other)
   if (f.mma) {
     f.dx = mma_shape(d.dtype, (uint32_t)rows, d.n_in, d.n_out);
     f.dw = mma_shape(d.dtype, d.n_in, d.n_out, (uint32_t)rows);

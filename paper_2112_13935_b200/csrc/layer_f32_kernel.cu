@@ -257,12 +257,10 @@ cudaError_t run(const MmaProduct& m, cudaStream_t s) {
   e = clusters_at_once(1, &slots);
   if (e != cudaSuccess) return e;
   const uint32_t items = L.tiles_m * L.tiles_n * L.splits;
-  kernel<<<items < slots ? items : slots, R::threads, R::total, s>>>(L, ma, mb);
-  e = cudaGetLastError();
+  e = launch_alone(kernel, dim3(items < slots ? items : slots), R::threads, R::total, 1, s, L, ma, mb);
   if (e != cudaSuccess || L.splits == 1) return e;
   const uint64_t groups = (uint64_t)m.p.m * ((m.p.n + 3) / 4);
-  split_sums_kernel<float><<<(unsigned)((groups + 255) / 256), 256, 0, s>>>(L.p, L.partial, L.ld_partial, L.splits);
-  return cudaGetLastError();
+  return launch(split_sums_kernel<float>, dim3((unsigned)((groups + 255) / 256)), 256, 0, 1, s, L.p, L.partial, L.ld_partial, L.splits);
 }
 
 }  // namespace

@@ -27,13 +27,14 @@ template <int TILE> struct Shape {
 };
 
 template <class TA, class TB, class Out, int TILE>
-__global__ void __launch_bounds__(kThreads) product_fma_kernel(const Product p, const uint32_t tiles_n) {
+__global__ void __launch_bounds__(kThreads, 2) product_fma_kernel(const Product p, const uint32_t tiles_n) {
   using S = Shape<TILE>;
   __shared__ __align__(16) float smem[4 * kStep * S::ld];
   float(*as)[kStep][S::ld] = reinterpret_cast<float(*)[kStep][S::ld]>(smem);
   float(*bs)[kStep][S::ld] = reinterpret_cast<float(*)[kStep][S::ld]>(smem + 2 * kStep * S::ld);
   float(*sums)[TILE][S::ld] = reinterpret_cast<float(*)[TILE][S::ld]>(smem);      // in the operands' place when they are done with
   static_assert(S::groups * TILE <= 4 * kStep, "the sums do not fit");
+  in_line();
   cg::cluster_group cluster = cg::this_cluster();
   const uint32_t split = cluster.num_blocks(), rank = cluster.block_rank();
   const uint32_t tile = blockIdx.x / split;
@@ -135,17 +136,8 @@ template <class TA, class TB, class Out>
 cudaError_t run(const Product& p, cudaStream_t s) {
   const bool wide = wide_tiles(p.m, p.n);
   const uint32_t tile = wide ? 64 : 32, split = fma_split(p.m, p.n, p.k), tiles_n = (uint32_t)(((uint64_t)p.n + tile - 1) / tile);
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(tiles_of(p.m, p.n, tile) * split));
-  cfg.blockDim = dim3(kThreads);
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = split;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, wide ? product_fma_kernel<TA, TB, Out, 64> : product_fma_kernel<TA, TB, Out, 32>, p, tiles_n);
+  return launch(wide ? product_fma_kernel<TA, TB, Out, 64> : product_fma_kernel<TA, TB, Out, 32>, dim3((unsigned)(tiles_of(p.m, p.n, tile) * split)), kThreads, 0,
+                split, s, p, tiles_n);
 }
 template <class T>
 cudaError_t of_type(const Product& p, cudaStream_t s) {     // a gradient's dz may be fp32 beside operands of T
@@ -162,6 +154,11 @@ uint32_t fma_split(uint32_t m, uint32_t n, uint32_t k) {
   uint32_t split = 1;
   while (split < 8 && tiles * split * 2 <= 2 * 148 && k >= 64 * 2 * split) split *= 2;
   return split;
+}
+
+uint64_t fma_volume(uint32_t m, uint32_t n, uint32_t k) {
+  const uint64_t tile = wide_tiles(m, n) ? 64 : 32;
+  return tiles_of(m, n, (uint32_t)tile) * tile * tile * k;
 }
 
 cudaError_t launch_product_fma(const Product& p, cudaStream_t s) {

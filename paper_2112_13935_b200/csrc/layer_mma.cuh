@@ -192,6 +192,7 @@ __device__ __forceinline__ void store_block(const Launch& L, uint32_t split, flo
 // The parts' sums of a split k, in their order, through the epilogue: four columns a thread.
 template <class Out>
 __global__ void __launch_bounds__(256) split_sums_kernel(const Product p, const float* partial, size_t ld, uint32_t splits) {
+  in_line();
   const uint32_t per = (p.n + 3) / 4;
   const uint64_t g = (uint64_t)blockIdx.x * 256 + threadIdx.x;
   if (g >= (uint64_t)per * p.m) return;

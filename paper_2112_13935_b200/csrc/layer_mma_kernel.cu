@@ -206,22 +206,10 @@ cudaError_t run(const MmaProduct& m, cudaStream_t s) {
   e = clusters_at_once(CG, &slots);
   if (e != cudaSuccess) return e;
   const uint32_t items = L.tiles_m * L.tiles_n * L.splits;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((items < slots ? items : slots) * CG);
-  cfg.blockDim = dim3(R::threads);
-  cfg.dynamicSmemBytes = R::total;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = CG;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, kernel, L, ma, mb);
+  e = launch_alone(kernel, dim3((items < slots ? items : slots) * CG), R::threads, R::total, CG, s, L, ma, mb);
   if (e != cudaSuccess || L.splits == 1) return e;
   const uint64_t groups = (uint64_t)m.p.m * ((m.p.n + 3) / 4);
-  split_sums_kernel<Out><<<(unsigned)((groups + 255) / 256), 256, 0, s>>>(L.p, L.partial, L.ld_partial, L.splits);
-  return cudaGetLastError();
+  return launch(split_sums_kernel<Out>, dim3((unsigned)((groups + 255) / 256)), 256, 0, 1, s, L.p, L.partial, L.ld_partial, L.splits);
 }
 
 template <class Out>
@@ -231,10 +219,12 @@ cudaError_t run(const MmaProduct& m, cudaStream_t s) {
 
 }  // namespace
 
-// The tensor cores take a product of 2^26 multiplications and more (below that their set-up costs more than the FMAs), and one whose tiles
-// are so few that the FMA kernel's clusters would go down more than 512 of k each.
-bool mma_takes(uint32_t m, uint32_t n, uint32_t k) {
-  return (uint64_t)m * n * k >= (uint64_t)1 << 26 || k / fma_split(m, n, k) > 512;
+// The tensor cores take a product from so many multiplications on (in whole tiles of the FMA kernel), and one whose tiles are so few that
+// that kernel's clusters would go down more than 512 of k each.  Both kernels in us on either side: bf16 256^3 (2^24) 7.7 here, 6.9 there,
+// 512 x 512 x 256 (2^26) 9.2 and 12.8; fp32, which needs a pass for the parts and six products, 512 x 512 x 256 18.4 and 12.0, 512^3 (2^27)
+// 19.0 and 19.5; fp32 60,000 x 128 x 10, in whole tiles 2^28.9, 19.5 and 47.
+bool mma_takes(uint32_t type, uint32_t m, uint32_t n, uint32_t k) {
+  return fma_volume(m, n, k) >= (type == kF32 ? 1ull << 27 : 1ull << 25) || k / fma_split(m, n, k) > 512;
 }
 MmaShape mma_shape(uint32_t type, uint32_t m, uint32_t n, uint32_t k) {
   MmaShape r{};

@@ -45,6 +45,7 @@ struct Product {
 // Small products, on FMAs (see layer_fma_kernel.cu).
 cudaError_t launch_product_fma(const Product& p, cudaStream_t s);
 uint32_t fma_split(uint32_t m, uint32_t n, uint32_t k);    // CTAs along k
+uint64_t fma_volume(uint32_t m, uint32_t n, uint32_t k);   // multiplications, in whole tiles
 
 // Up to eight rows of A along k against a B across it (see layer_rows_kernel.cu).
 bool rows_kernel_takes(uint32_t m, uint32_t k);
@@ -69,7 +70,7 @@ struct MmaProduct {
   MmaShape shape;
   float* partial;    // mma_partial_floats() of workspace
 };
-bool mma_takes(uint32_t m, uint32_t n, uint32_t k);   // rather than the FMA kernel
+bool mma_takes(uint32_t type, uint32_t m, uint32_t n, uint32_t k);   // rather than the FMA kernel
 MmaShape mma_shape(uint32_t type, uint32_t m, uint32_t n, uint32_t k);
 size_t mma_partial_floats(const MmaShape& s, uint32_t m, uint32_t n);
 cudaError_t launch_product_mma(const MmaProduct& m, cudaStream_t s);

@@ -26,6 +26,7 @@ __global__ void __launch_bounds__(kThreads) product_rows_kernel(const Product p,
   extern __shared__ __align__(16) float smem[];
   float* xs = smem;                      // [R][kc]
   float* sums = smem + R * kc;           // [kWarps][R][kCols]
+  in_line();
   cg::cluster_group cluster = cg::this_cluster();
   const uint32_t split = cluster.num_blocks(), rank = cluster.block_rank();
   const uint32_t n0 = blockIdx.x / split * kCols, k0 = rank * kc;
@@ -122,18 +123,7 @@ cudaError_t go(const Product& p, cudaStream_t s) {
   const size_t smem = ((size_t)R * kc + (size_t)kWarps * R * kCols) * 4;
   const auto kernel = product_rows_kernel<T, Out, R, kVec>;
   if (const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024)) return e;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(across * split));
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = split;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, p, kc);
+  return launch(kernel, dim3((unsigned)(across * split)), kThreads, smem, split, s, p, kc);
 }
 template <class T, class Out>
 cudaError_t run(const Product& p, cudaStream_t s) {

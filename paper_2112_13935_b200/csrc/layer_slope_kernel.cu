@@ -25,6 +25,7 @@ __device__ __forceinline__ void store_wide(float* p, bool whole, int n, const fl
 template <class T, int N, bool kVec>
 __global__ void __launch_bounds__(kThreads, 4) slope_kernel(const SlopeLaunch p, const uint32_t slabs, const uint32_t log) {
   __shared__ __align__(16) float sums[kThreads * N];
+  in_line();
   const uint32_t lane = threadIdx.x & ((1u << log) - 1), down = threadIdx.x >> log, at_once = kThreads >> log;
   const uint32_t col = ((blockIdx.x << log) + lane) * N;
   const size_t r_from = (size_t)p.rows * blockIdx.y / slabs, r_to = (size_t)p.rows * (blockIdx.y + 1) / slabs;
@@ -92,6 +93,7 @@ __global__ void __launch_bounds__(kThreads, 4) slope_kernel(const SlopeLaunch p,
 template <class T>
 __global__ void __launch_bounds__(256) slab_sums_kernel(const float* partial, uint32_t slabs, uint32_t cols, T* db, uint32_t accumulate) {
   __shared__ float sums[8][32];
+  in_line();
   const int lane = threadIdx.x % 32, part = threadIdx.x / 32;
   const uint32_t c = blockIdx.x * 32 + lane;
   float v = 0.f;
@@ -120,25 +122,23 @@ uint32_t slabs_of(uint32_t rows, uint32_t cols) {
 bool aligned(const void* p, size_t ld, size_t n, size_t bytes) { return !p || ((uintptr_t)p % (n * bytes) == 0 && ld % n == 0); }
 
 template <class T, int N, bool kVec>
-void go(const SlopeLaunch& p, uint32_t slabs, cudaStream_t s) {
+cudaError_t go(const SlopeLaunch& p, uint32_t slabs, cudaStream_t s) {
   const uint32_t log = log_lanes<N>(p.cols);
   const uint64_t across = (((uint64_t)p.cols + N - 1) / N + (1u << log) - 1) >> log;
-  slope_kernel<T, N, kVec><<<dim3((unsigned)across, slabs), kThreads, 0, s>>>(p, slabs, log);
+  return launch(slope_kernel<T, N, kVec>, dim3((unsigned)across, slabs), kThreads, 0, 1, s, p, slabs, log);
 }
 template <class T>
 cudaError_t run(const SlopeLaunch& p, cudaStream_t s) {
   constexpr int N = 16 / (int)sizeof(T);
   const uint32_t slabs = slabs_of(p.rows, p.cols);
   const bool vec = aligned(p.dy, p.ld_dy, N, sizeof(T)) && aligned(p.pre, p.ld_pre, N, sizeof(T)) && aligned(p.dz, p.ld_dz, N, type_bytes(p.dz_type));
-  if (vec) go<T, N, true>(p, slabs, s);
-  else go<T, 4, false>(p, slabs, s);
-  if (p.db) {
-    const uint32_t grid = (p.cols + 31) / 32;
-    if (p.db_type == kF32) slab_sums_kernel<<<grid, 256, 0, s>>>(p.partial, slabs, p.cols, static_cast<float*>(p.db), p.accumulate);
-    else if (p.db_type == kBf16) slab_sums_kernel<<<grid, 256, 0, s>>>(p.partial, slabs, p.cols, static_cast<__nv_bfloat16*>(p.db), p.accumulate);
-    else slab_sums_kernel<<<grid, 256, 0, s>>>(p.partial, slabs, p.cols, static_cast<__half*>(p.db), p.accumulate);
-  }
-  return cudaGetLastError();
+  const cudaError_t e = vec ? go<T, N, true>(p, slabs, s) : go<T, 4, false>(p, slabs, s);
+  if (e != cudaSuccess || !p.db) return e;
+  const dim3 grid((p.cols + 31) / 32);
+  if (p.db_type == kF32) return launch(slab_sums_kernel<float>, grid, 256, 0, 1, s, p.partial, slabs, p.cols, static_cast<float*>(p.db), p.accumulate);
+  if (p.db_type == kBf16)
+    return launch(slab_sums_kernel<__nv_bfloat16>, grid, 256, 0, 1, s, p.partial, slabs, p.cols, static_cast<__nv_bfloat16*>(p.db), p.accumulate);
+  return launch(slab_sums_kernel<__half>, grid, 256, 0, 1, s, p.partial, slabs, p.cols, static_cast<__half*>(p.db), p.accumulate);
 }
 
 }  // namespace

@@ -189,6 +189,7 @@ template <class T> __device__ __forceinline__ void no_answer(const LossLaunch& p
 // Short rows: G lanes a row, NV pieces a lane.
 template <class T, int G, int NV>
 __global__ void __launch_bounds__(kThreads) loss_lanes_kernel(const LossLaunch p) {
+  in_line();
   const size_t row = ((size_t)blockIdx.y * gridDim.x + blockIdx.x) * (kThreads / G) + threadIdx.x / G;
   const int lane = threadIdx.x % G;
   const bool here = row < p.rows;
@@ -244,6 +245,7 @@ __global__ void __launch_bounds__(kThreads) loss_cluster_kernel(const LossLaunch
   __shared__ Part ctas[8];
   __shared__ float tops[kThreads / 32], sums[kThreads / 32];
   __shared__ int32_t firsts[kThreads / 32];
+  in_line();
   // (width is a power of two; no division)
   const uint32_t width = 1u << log_width, rank = blockIdx.x & (width - 1);
   const size_t row = (size_t)blockIdx.y * (gridDim.x >> log_width) + (blockIdx.x >> log_width);
@@ -336,8 +338,7 @@ constexpr uint64_t kMostX = 1u << 20;     // CTAs along x; the rest along y
 template <class T, int G, int NV>
 cudaError_t lanes(const LossLaunch& p, cudaStream_t s) {
   const uint64_t ctas = (p.rows + kThreads / G - 1) / (kThreads / G), x = ctas < kMostX ? ctas : kMostX;
-  loss_lanes_kernel<T, G, NV><<<dim3((unsigned)x, (unsigned)((ctas + x - 1) / x)), kThreads, 0, s>>>(p);
-  return cudaGetLastError();
+  return launch(loss_lanes_kernel<T, G, NV>, dim3((unsigned)x, (unsigned)((ctas + x - 1) / x)), kThreads, 0, 1, s, p);
 }
 constexpr uint64_t kPieces = 4096, kMostPieces = 13 * 1024;     // of a CTA: 64 KB, so that three share an SM; 208 KB
 
@@ -345,20 +346,10 @@ template <class T, bool kOnce>
 cudaError_t ctas(const LossLaunch& p, uint32_t width, uint64_t pieces, cudaStream_t s) {
   const auto kernel = loss_cluster_kernel<T, kOnce>;
   const uint64_t most = kMostX / width, x = p.rows < most ? p.rows : most;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(x * width), (unsigned)((p.rows + x - 1) / x));
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = kOnce ? (pieces + width - 1) / width * 16 : 0;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = width;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
   if (kOnce)
     if (const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kMostPieces * 16))) return e;
-  return cudaLaunchKernelEx(&cfg, kernel, p, width == 8 ? 3u : width / 2);
+  return launch(kernel, dim3((unsigned)(x * width), (unsigned)((p.rows + x - 1) / x)), kThreads, kOnce ? (pieces + width - 1) / width * 16 : 0, width, s, p,
+                width == 8 ? 3u : width / 2);
 }
 
 template <class T>
