@@ -357,7 +357,10 @@ aet_status aet_round_no_alloc(const aet_config* cfg, uint32_t client, uint32_t r
  * as there are columns), from an address that is a multiple of the element size.
  * Sums, activations and statistics are held in fp32; a value is rounded to the
  * element type (to nearest even) where it is stored.  The same call gives the same
- * bits.  Errors: AET_ERR_ARG, AET_ERR_CUDA; text by aet_last_error(NULL).  */
+ * bits.  A bounded device-side wait that gives up leaves NaN.  Rows and columns
+ * up to 2^31 - 1, an ld up to 2^31, offsets of 64 bits.  The calls may come from any
+ * thread; a stream of the current device.  Errors: AET_ERR_ARG, AET_ERR_CUDA; text by
+ * aet_last_error(NULL).  */
 typedef enum { AET_F32 = 0, AET_BF16 = 1, AET_F16 = 2 } aet_dtype;
 typedef enum {
   AET_ACT_NONE = 0,
@@ -392,8 +395,8 @@ aet_status aet_dropout(uint32_t dtype, size_t rows, uint32_t cols, const aet_dro
  *   dlogits[r] = scale * weight[r] * (softmax(z) - 1_label)        (dtype)
  *   top[r]     = the lowest index of the row's maximum
  * loss, dlogits, top and weight (1 each) may be null; dlogits may be the logits
- * (same ld).  A negative label means a row without an answer: loss and gradient 0,
- * top -1, whatever its logits hold.  -inf logits are classes that cannot be.  A row
+ * (same ld); up to 2^30 classes.  A negative label means a row without an answer: loss
+ * and gradient 0, top -1, whatever its logits hold.  -inf logits are classes that cannot be.  A row
  * that holds NaN or +inf, or -inf only, or whose label is >= classes, has loss and
  * gradient NaN; top is -1 where the row holds a NaN. */
 aet_status aet_cross_entropy(uint32_t dtype, size_t rows, uint32_t classes, const void* logits, size_t ld,

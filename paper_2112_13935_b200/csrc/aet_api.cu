@@ -942,6 +942,8 @@ aet_status run_evaluation(aet_handle* h, uint32_t node, const float* x, const in
   Tally* tally = reinterpret_cast<Tally*>(ws + o_tally);
   float* g = gradient ? reinterpret_cast<float*>(ws + o_grad) : nullptr;
   h->last_stream = s;
+  AET_CUDA(h, cudaStreamSynchronize(s));     // what earlier runs report comes before anything is written
+  if (aet_status ds = check_device_status(h)) return ds;
   AET_CUDA(h, cudaMemsetAsync(tally, 0, sizeof(Tally), s));
   for (size_t r = 0; r < n; r += chunk) {
     const size_t rows = n - r < chunk ? n - r : chunk;
@@ -963,7 +965,6 @@ aet_status run_evaluation(aet_handle* h, uint32_t node, const float* x, const in
   Tally t{};
   AET_CUDA(h, cudaMemcpyAsync(&t, tally, sizeof(t), cudaMemcpyDefault, s));
   AET_CUDA(h, cudaStreamSynchronize(s));
-  if (aet_status ds = check_device_status(h)) return ds;
   if (!y) return AET_OK;
   if (t.bad_labels) return fail(h, AET_ERR_ARG, "a label is out of range");
   t.loss /= (double)n;

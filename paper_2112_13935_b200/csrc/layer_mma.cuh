@@ -15,7 +15,7 @@ namespace {
 
 constexpr int kBlock = 16;         // columns that go through a warp's buffer at once
 
-constexpr uint32_t kWaitLimit = 1u << 22;
+constexpr unsigned long long kWaitNs = 4000000000ull;
 constexpr uint32_t kGroup = 16;     // tile rows that are walked together, so that their operands meet in L2
 
 struct Launch {
@@ -34,14 +34,21 @@ __device__ __forceinline__ bool elect_one() {
 }
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count)); }
+// Waits, but not for ever: the longest wait there is, for the sums of a k of 2^31 in 32 parts, takes about half a second.
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
-  for (uint32_t i = 0; i < kWaitLimit; ++i) {
+  unsigned long long from = 0;
+  for (uint32_t i = 1;; ++i) {
     uint32_t ok;
     asm volatile("{\n\t.reg .pred q;\n\tmbarrier.try_wait.parity.shared::cta.b64 q, [%1], %2;\n\tselp.u32 %0, 1, 0, q;\n\t}"
                  : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     if (ok) return true;
+    if (i % 1024 == 0) {
+      unsigned long long now;
+      asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
+      if (!from) from = now;
+      if (now - from > kWaitNs) return false;
+    }
   }
-  return false;
 }
 __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");

@@ -434,3 +434,103 @@ def test_a_training_step_repeats_bit_for_bit_on_streams_and_in_graphs():
         torch.cuda.synchronize()
     for st, w in zip(states, want):
         assert all(torch.equal(w[k], st[3][k]) for k in w)
+
+
+# ---- offsets past 32 bits, first calls in a capture -----------------------------------------------------------------------
+
+def far(rows, cols, ld, dtype, values=None):
+    """A matrix whose last row starts more than 2^31 elements behind its first."""
+    assert (rows - 1) * ld >= 2 ** 31
+    m = torch.empty((rows - 1) * ld + cols, dtype=dtype, device="cuda").as_strided((rows, cols), (ld, 1))
+    if values is not None:
+        m.copy_(values)
+    return m
+
+
+@pytest.mark.parametrize("rows,n_in,n_out,type", [(3, 200, 90, "bf16"), (20, 70, 33, "bf16"), (130, 640, 900, "f16"), (130, 1024, 1100, "f32")])
+def test_dense_of_rows_far_apart(rows, n_in, n_out, type):
+    """Few rows, FMAs, tensor cores: the same bits as with rows side by side."""
+    t = lh.TYPES[type]
+    ld = -(-2 ** 31 // (rows - 1)) // 8 * 8 + 8
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, w, dy = (torch.randn(a, b, generator=g, device="cuda").to(t) for a, b in ((rows, n_in), (n_in, n_out), (rows, n_out)))
+    near = api.aet_dense(n_in, n_out, dtype=t, act="silu")
+    apart = api.aet_dense(n_in, n_out, dtype=t, act="silu", ld_x=ld, ld_pre=ld)
+    got = []
+    for plan, xx, pre in ((near, x, torch.empty(rows, n_out, dtype=t, device="cuda")), (apart, far(rows, n_in, ld, t, x), far(rows, n_out, ld, t))):
+        y, dx, dw = torch.empty_like(dy), torch.empty_like(x), torch.empty_like(w)
+        api.aet_dense_forward(plan, xx, w, None, y, pre=pre, workspace=workspace(plan, rows, False))
+        api.aet_dense_backward(plan, xx, w, dy, pre=pre, dx=dx, dw=dw, workspace=workspace(plan, rows, True))
+        got.append((y, pre, dx, dw))
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+
+
+def test_loss_and_dropout_of_rows_far_apart():
+    ld, t = 2 ** 30 + 4, torch.bfloat16
+    g = torch.Generator(device="cuda").manual_seed(2)
+    z = torch.randn(3, 1001, generator=g, device="cuda").to(t)
+    labels = torch.tensor([3, 0, 1000], dtype=torch.int32, device="cuda")
+    zz = far(3, 1001, ld, t, z)
+    out = []
+    for m in (z, zz):
+        loss, grad = torch.empty(3, device="cuda"), torch.empty(3, 1001, dtype=t, device="cuda")
+        api.aet_cross_entropy(m, labels, loss=loss, dlogits=grad)
+        y = torch.empty(3, 1001, dtype=t, device="cuda")
+        api.aet_dropout(api.aet_dropout_spec(1, rate=0.5), m, y)
+        out.append((loss, grad, y))
+    for a, b in zip(*out):
+        assert torch.equal(a, b)
+    api.aet_cross_entropy(zz, labels, dlogits=zz)
+    assert torch.equal(zz, out[0][1])
+
+
+FIRST_CALLS = """
+import sys, torch
+sys.path[:0] = [%r]
+from paper_2112_13935_b200 import api
+t = torch.bfloat16
+x, w, dy = (torch.ones(a, b, dtype=t, device='cuda') for a, b in ((512, 768), (768, 640), (512, 640)))
+plan = api.aet_dense(768, 640, dtype=t, act='relu')
+ws = [torch.empty(api.aet_dense_workspace(plan, 512, b), dtype=torch.uint8, device='cuda') for b in (False, True)]
+y, dx, dw, db = dy.clone(), x.clone(), w.clone(), dy[0].clone()
+labels, grad = torch.zeros(512, dtype=torch.int32, device='cuda'), dy.clone()
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    api.aet_dense_forward(plan, x, w, None, y, workspace=ws[0])
+    api.aet_cross_entropy(y, labels, dlogits=grad)
+    api.aet_dense_backward(plan, x, w, dy, pre=y, dx=dx, dw=dw, db=db, workspace=ws[1])
+    api.aet_dropout(api.aet_dropout_spec(1, rate=0.5), dx, dx)
+g.replay()
+torch.cuda.synchronize()
+assert (y == 768).all() and (dw == 512).all() and (db == 512).all() and set(dx.unique().tolist()) == {0.0, 1280.0}
+print('fine')
+"""
+
+
+def test_first_calls_of_a_process_inside_a_capture():
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS % root], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "fine" in r.stdout, r.stderr[-2000:]
+
+
+def test_two_streams_at_once():
+    """Calls that overlap on the GPU, each with its own workspace, give what they give alone."""
+    states = [step_state(700, (900, 640, 70), torch.bfloat16, seed, 0.2) for seed in (1, 2)]
+    want = []
+    for st in states:
+        training_step(*st)
+        torch.cuda.synchronize()
+        want.append({k: v.clone() for k, v in st[3].items()})
+    streams = [torch.cuda.Stream() for _ in states]
+    for _ in range(5):
+        for st, s in zip(states, streams):
+            with torch.cuda.stream(s):
+                training_step(*st)
+    torch.cuda.synchronize()
+    for st, w in zip(states, want):
+        assert all(torch.equal(w[k], st[3][k]) for k in w)
