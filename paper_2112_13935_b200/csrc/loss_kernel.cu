@@ -239,12 +239,12 @@ __global__ void __launch_bounds__(kThreads) loss_lanes_kernel(const LossLaunch p
 
 // Long rows: a cluster of CTAs (or one) a row.  The pieces wait in shared memory (kOnce; a thread reads back what it copied itself, so that
 // nobody waits for anyone), where three short loops pass over them; in registers, eight pieces a thread were spilled (1.75 ms for the rows above).
-template <class T, bool kOnce>
-__global__ void __launch_bounds__(kThreads) loss_cluster_kernel(const LossLaunch p, const uint32_t log_width) {
+template <class T, bool kOnce, int THREADS>
+__global__ void __launch_bounds__(THREADS) loss_cluster_kernel(const LossLaunch p, const uint32_t log_width) {
   extern __shared__ uint4 mine[];
   __shared__ Part ctas[8];
-  __shared__ float tops[kThreads / 32], sums[kThreads / 32];
-  __shared__ int32_t firsts[kThreads / 32];
+  __shared__ float tops[THREADS / 32], sums[THREADS / 32];
+  __shared__ int32_t firsts[THREADS / 32];
   in_line();
   // (width is a power of two; no division)
   const uint32_t width = 1u << log_width, rank = blockIdx.x & (width - 1);
@@ -253,7 +253,7 @@ __global__ void __launch_bounds__(kThreads) loss_cluster_kernel(const LossLaunch
   const int tid = threadIdx.x;
   const int32_t y = p.labels[row];
   if (y < 0) {
-    no_answer<T>(p, row, rank * kThreads + tid, width * kThreads);
+    no_answer<T>(p, row, rank * THREADS + tid, width * THREADS);
     return;
   }
   if (width > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");    // I run: the others may push
@@ -262,12 +262,12 @@ __global__ void __launch_bounds__(kThreads) loss_cluster_kernel(const LossLaunch
   const int32_t per = (r.count + (int32_t)width - 1) >> log_width, q0 = (int32_t)rank * per, q1 = min(r.count, q0 + per);
   if (kOnce) {
     const uint32_t to = (uint32_t)__cvta_generic_to_shared(mine);
-    for (int32_t c = q0 + tid; c < q1; c += kThreads)
+    for (int32_t c = q0 + tid; c < q1; c += THREADS)
       asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + 16 * (uint32_t)(c - q0)), "l"(r.pieces + c) : "memory");
     asm volatile("cp.async.wait_all;" ::: "memory");
     for (int32_t e = 0; e < 2; ++e) {     // the row's first and last pieces, by who copied them
       const int32_t c = e ? r.count - 1 : 0;
-      if (c >= q0 && c < q1 && (c - q0) % kThreads == tid) trim(r, mine[c - q0], c);
+      if (c >= q0 && c < q1 && (c - q0) % THREADS == tid) trim(r, mine[c - q0], c);
     }
   }
   const float zy = logit(p, z, y);
@@ -280,7 +280,7 @@ __global__ void __launch_bounds__(kThreads) loss_cluster_kernel(const LossLaunch
   float top = -CUDART_INF_F, sum = 0.f;
   int32_t first = kNone;
 #pragma unroll 4
-  for (int32_t c = q0 + tid; c < q1; c += kThreads) {
+  for (int32_t c = q0 + tid; c < q1; c += THREADS) {
     const float m = largest<T>(piece(c));
     if (m > top) top = m, first = c;
   }
@@ -289,10 +289,10 @@ __global__ void __launch_bounds__(kThreads) loss_cluster_kernel(const LossLaunch
   if (tid % 32 == 0) tops[tid / 32] = a.top;
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kThreads / 32; ++i) a.top = fmaxf(a.top, tops[i]);
+  for (int i = 0; i < THREADS / 32; ++i) a.top = fmaxf(a.top, tops[i]);
   const Base b = base_of(a.top);
 #pragma unroll 2
-  for (int32_t c = q0 + tid; c < q1; c += kThreads) sum += powers<T>(piece(c), b);
+  for (int32_t c = q0 + tid; c < q1; c += THREADS) sum += powers<T>(piece(c), b);
   sum = lanes_sum<32>(sum);
   first = p.top ? lanes_min<32>(top == a.top ? first : kNone) : 0;
   if (tid % 32 == 0) sums[tid / 32] = sum, firsts[tid / 32] = first;
@@ -300,7 +300,7 @@ __global__ void __launch_bounds__(kThreads) loss_cluster_kernel(const LossLaunch
   a.sum = 0.f;
   a.at = kNone;
 #pragma unroll
-  for (int i = 0; i < kThreads / 32; ++i) a.sum += sums[i], a.at = min(a.at, firsts[i]);
+  for (int i = 0; i < THREADS / 32; ++i) a.sum += sums[i], a.at = min(a.at, firsts[i]);
   if (width > 1) {
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     if (tid < (int)width) *cg::this_cluster().map_shared_rank(&ctas[rank], tid) = a;
@@ -314,23 +314,23 @@ __global__ void __launch_bounds__(kThreads) loss_cluster_kernel(const LossLaunch
     a.at = lanes_min<8>(b.top == a.top ? b.at : kNone);
   }
   if (rank == 0 && tid == 0) write_loss(p, row, a, zy);
-  if (p.top && a.at >= q0 && a.at < q1 && (a.at - q0) % kThreads == tid) write_top(p, r, row, a, piece(a.at), a.at);
+  if (p.top && a.at >= q0 && a.at < q1 && (a.at - q0) % THREADS == tid) write_top(p, r, row, a, piece(a.at), a.at);
   if (!p.grad) return;
   const Slope<T> s(p, row, y, a, r.shift);
   if (s.whole) {
     const int32_t i0 = r.ragged(0), i1 = r.count - r.ragged(r.count - 1);     // pieces within [i0, i1) are the row's alone
 #pragma unroll 2
-    for (int32_t c = q0 + tid; c < q1; c += kThreads)
+    for (int32_t c = q0 + tid; c < q1; c += THREADS)
       if (c >= i0 && c < i1) write_grad(r, piece(c), c, s, true);
     for (int32_t e = 0; e < 2; ++e) {
       const int32_t c = e ? r.count - 1 : 0;
-      if (r.ragged(c) && c >= q0 && c < q1 && (c - q0) % kThreads == tid) write_grad(r, piece(c), c, s, false);
+      if (r.ragged(c) && c >= q0 && c < q1 && (c - q0) % THREADS == tid) write_grad(r, piece(c), c, s, false);
     }
   } else {
-    for (int32_t c = q0 + tid; c < q1; c += kThreads) write_grad(r, piece(c), c, s, false);
+    for (int32_t c = q0 + tid; c < q1; c += THREADS) write_grad(r, piece(c), c, s, false);
   }
   const int32_t at = label_piece(r, y);
-  if (at >= q0 && at < q1 && (at - q0) % kThreads == tid) write_label(s, zy);
+  if (at >= q0 && at < q1 && (at - q0) % THREADS == tid) write_label(s, zy);
 }
 
 constexpr uint64_t kMostX = 1u << 20;     // CTAs along x; the rest along y
@@ -342,13 +342,13 @@ cudaError_t lanes(const LossLaunch& p, cudaStream_t s) {
 }
 constexpr uint64_t kPieces = 4096, kMostPieces = 13 * 1024;     // of a CTA: 64 KB, so that three share an SM; 208 KB
 
-template <class T, bool kOnce>
+template <class T, bool kOnce, int THREADS>
 cudaError_t ctas(const LossLaunch& p, uint32_t width, uint64_t pieces, cudaStream_t s) {
-  const auto kernel = loss_cluster_kernel<T, kOnce>;
+  const auto kernel = loss_cluster_kernel<T, kOnce, THREADS>;
   const uint64_t most = kMostX / width, x = p.rows < most ? p.rows : most;
   if (kOnce)
     if (const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kMostPieces * 16))) return e;
-  return launch(kernel, dim3((unsigned)(x * width), (unsigned)((p.rows + x - 1) / x)), kThreads, kOnce ? (pieces + width - 1) / width * 16 : 0, width, s, p,
+  return launch(kernel, dim3((unsigned)(x * width), (unsigned)((p.rows + x - 1) / x)), THREADS, kOnce ? (pieces + width - 1) / width * 16 : 0, width, s, p,
                 width == 8 ? 3u : width / 2);
 }
 
@@ -361,11 +361,15 @@ cudaError_t run(const LossLaunch& p, cudaStream_t s) {
   if (pieces <= 32) return lanes<T, 32, 1>(p, s);
   if (pieces <= 64) return lanes<T, 32, 2>(p, s);
   if (pieces <= 128) return lanes<T, 32, 4>(p, s);
-  // sixteen pieces a thread and the CTAs that takes; few rows: more CTAs, with as few as two pieces a thread
+  if (pieces <= 256) return lanes<T, 32, 8>(p, s);
+  // eight pieces and more a thread, as far as there are rows enough to fill the SMs with small CTAs
+  if (p.rows >= 148 * 16 && pieces <= 512) return ctas<T, true, 64>(p, 1, pieces, s);
+  if (p.rows >= 148 * 8 && pieces <= 1024) return ctas<T, true, 128>(p, 1, pieces, s);
+  // up to sixteen pieces a thread and the CTAs that takes; few rows: more CTAs, with as few as two pieces a thread
   uint32_t width = 1;
   while (width < 8 && (pieces > kPieces * width || (p.rows * width * 2 <= 148 && pieces > 2ull * kThreads * width))) width *= 2;
-  if (pieces <= kMostPieces * width) return ctas<T, true>(p, width, pieces, s);
-  return ctas<T, false>(p, width, pieces, s);
+  if (pieces <= kMostPieces * width) return ctas<T, true, kThreads>(p, width, pieces, s);
+  return ctas<T, false, kThreads>(p, width, pieces, s);
 }
 
 }  // namespace

@@ -263,7 +263,7 @@ def check_loss(z, labels, type, scale=1.0, weight=None, pad=0, shift=0, in_place
 
 
 @pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
-@pytest.mark.parametrize("rows,n", [(1, 1), (3, 2), (7, 10), (300, 10), (33, 31), (40, 33), (9, 100), (5, 257), (3, 1000), (2, 1025), (3, 4099), (2, 30001), (1, 131072), (200, 9000), (1, 300007), (1, 1000003)])
+@pytest.mark.parametrize("rows,n", [(1, 1), (3, 2), (7, 10), (300, 10), (33, 31), (40, 33), (9, 100), (5, 257), (3, 1000), (2, 1025), (3, 4099), (2, 30001), (1, 131072), (200, 9000), (1, 300007), (1, 1000003), (2400, 3000), (1200, 5003)])
 def test_loss_sizes(rows, n, type):
     r = np.random.default_rng(rows * 1000 + n)
     z = r.standard_normal((rows, n)) * 2
