@@ -98,14 +98,11 @@ __global__ void __launch_bounds__((Ring<BN>::threads), 1) product_f32_kernel(con
           } else {
             tma_load<1>(a, &map_a, bar, k0, m0, 0);
           }
+          if (L.b_mn) {
 #pragma unroll
-          for (int q = 0; q < 3; ++q) {
-            if (L.b_mn) {
-#pragma unroll
-              for (int c = 0; c < BN / 64; ++c) tma_load<1>(b + q * R::b_part + c * R::b_block, &map_b, bar, n0 + c * 64, k0, q);
-            } else {
-              tma_load<1>(b + q * R::b_part, &map_b, bar, k0, n0, q);
-            }
+            for (int c = 0; c < BN / 64; ++c) tma_load<1>(b + 3 * c * R::b_block, &map_b, bar, n0 + c * 64, k0, 0);
+          } else {
+            tma_load<1>(b, &map_b, bar, k0, n0, 0);
           }
         }
       }
@@ -117,7 +114,7 @@ __global__ void __launch_bounds__((Ring<BN>::threads), 1) product_f32_kernel(con
     if (elect_one()) {
       uint32_t it = 0, ac = 0;
       bool ok = true;
-      const uint32_t b_step = L.b_mn ? 2048 >> 4 : 32 >> 4;
+      const uint32_t b_step = L.b_mn ? 2048 >> 4 : 32 >> 4, b_plane = (L.b_mn ? R::b_block : R::b_part) >> 4;     // of k, of the parts
       for (uint32_t item = blockIdx.x; item < items && ok; item += gridDim.x) {
         const Tile t = tile_of(L, item, kbs);
         for (uint32_t kb = t.kb0; kb < t.kb1 && ok; ++ac) {
@@ -131,14 +128,14 @@ __global__ void __launch_bounds__((Ring<BN>::threads), 1) product_f32_kernel(con
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t a = tmem_a + s * R::a_cols;
-            const uint64_t b = tile_desc<R::bk>(base + s * R::stage + R::a_bytes, L.b_mn);
+            const uint64_t b = tile_desc<R::bk, 3>(base + s * R::stage + R::a_bytes, L.b_mn);
             // small products first: low x high and middle x middle, then middle x high, then high x high
             constexpr int pa[6] = {2, 1, 0, 1, 0, 0}, pb[6] = {0, 1, 2, 0, 1, 0};
 #pragma unroll
             for (int q = 0; q < 6; ++q)
 #pragma unroll
               for (int k = 0; k < R::bk / 16; ++k) {
-                mma_a_tmem(d, a + pa[q] * (R::bk / 2) + k * 8, (uint32_t)b + pb[q] * (R::b_part >> 4) + k * b_step, (uint32_t)(b >> 32), L.idesc, accumulate);
+                mma_a_tmem(d, a + pa[q] * (R::bk / 2) + k * 8, (uint32_t)b + pb[q] * b_plane + k * b_step, (uint32_t)(b >> 32), L.idesc, accumulate);
                 accumulate = 1;
               }
             commit<1>(empty + 8 * s);

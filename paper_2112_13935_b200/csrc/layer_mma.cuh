@@ -121,10 +121,10 @@ __device__ __forceinline__ void tmem_wait(uint32_t (&r)[N][kBlock]) {
     for (int i = 0; i < kBlock; ++i) asm volatile("" : "+r"(r[c][i]));     // (no use of a value moves in front of the wait)
 }
 // Matrix descriptor of a swizzled tile.  Along k: rows of bk elements (128 or 64 bytes, swizzled as wide), 8-row groups one after another.
-// Across k: 128-byte rows of 64 of M or N, bk of them to a block, blocks one after another, in them 8 of k every 1,024 bytes.
-template <int bk>
+// Across k: 128-byte rows of 64 of M or N, bk of them to a block, blocks one after another (of as many planes), in them 8 of k every 1,024 bytes.
+template <int bk, int planes = 1>
 __device__ __forceinline__ uint64_t tile_desc(uint32_t addr, bool mn) {
-  const uint32_t lead = mn ? 64 * bk * 2 : 16, stride = mn || bk == 64 ? 1024 : 512;
+  const uint32_t lead = mn ? planes * 64 * bk * 2 : 16, stride = mn || bk == 64 ? 1024 : 512;
   const uint64_t swizzle = mn || bk == 64 ? 2 : 4;
   return (uint64_t)((addr & 0x3FFFF) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(stride >> 4) << 32 | (uint64_t)1 << 46 | swizzle << 61;
 }
@@ -231,14 +231,14 @@ inline Encode encoder() {
   return reinterpret_cast<Encode>(f);
 }
 
-// [planes][outer][inner] elements, boxes of box_cols x box_rows, swizzled as wide as a box's rows (128 or 64 bytes).
+// [planes][outer][inner] elements, boxes of box_cols x box_rows of all planes, swizzled as wide as a box's rows (128 or 64 bytes).
 inline cudaError_t encode(CUtensorMap* map, const MmaOperand& o, uint32_t type, uint32_t planes, uint64_t inner, uint64_t outer, uint32_t box_cols,
                           uint32_t box_rows) {
   const Encode f = encoder();
   if (!f) return cudaErrorNotSupported;
   const cuuint64_t dims[3] = {inner, outer, planes}, size = type == kF32 ? 4 : 2;
   const cuuint64_t strides[2] = {o.ld * size, (planes > 1 ? o.plane * size : (outer * o.ld * size + 15) / 16 * 16)};
-  const cuuint32_t box[3] = {box_cols, box_rows, 1}, steps[3] = {1, 1, 1};
+  const cuuint32_t box[3] = {box_cols, box_rows, planes}, steps[3] = {1, 1, 1};
   const CUresult r = f(map, type == kF32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : type == kF16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(o.p), dims, strides, box, steps,
                        CU_TENSOR_MAP_INTERLEAVE_NONE, box_cols * size == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
