@@ -366,7 +366,8 @@ typedef enum {
   AET_ACT_NONE = 0,
   AET_ACT_RELU = 1, /* derivative 0 at 0 */
   AET_ACT_GELU = 2, /* z Phi(z), Phi by the error function */
-  AET_ACT_SILU = 3  /* z / (1 + exp(-z)) */
+  AET_ACT_SILU = 3  /* z / (1 + exp(-z)); like AET_ACT_GELU, NaN at -inf and with a slope
+                       that is NaN at infinities (finite everywhere else) */
 } aet_act;
 
 /* Dropout with a mask that is a function of where an element stands and is never

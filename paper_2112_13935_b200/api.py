@@ -137,16 +137,35 @@ def aet_get_update_sum(h, seq: int, out=None, stream=None):
     return out
 
 
+def _kind(a, kind: str, what: str):
+    if str(a.dtype).rsplit(".", 1)[-1] != kind:
+        raise AetError(1, f"{what}: {a.dtype}, expected {kind}")
+
+
 def aet_predict(h, node: int, x, logits=None, classes=None, stream=None):
-    """Logits [n, classes] of a node's model for the rows of x; host or device arrays (logits default: a numpy array)."""
+    """Logits [n, classes] of a node's model for the rows of x; host or device arrays (without `logits` a numpy array of `classes` columns)."""
     if logits is None:
+        if classes is None:
+            raise AetError(1, "either logits or classes is needed")
         logits = np.empty((x.shape[0], classes), dtype=np.float32)
+    _kind(x, "float32", "x")
+    _kind(logits, "float32", "logits")
+    if logits.shape[0] != x.shape[0]:
+        raise AetError(1, f"logits: {logits.shape[0]} rows for {x.shape[0]}")
     _check(h, _lib.load().aet_predict(h, node, _ptr(x), x.shape[0], _ptr(logits), _stream(stream)))
     return logits
 
 
 def aet_evaluate(h, node: int, x, y, dropout=None, gradient=None, stream=None):
     """(loss, rows the model gets right) of a node's model on rows x with classes y; gradient: where the loss's gradient goes."""
+    _kind(x, "float32", "x")
+    _kind(y, "int32", "y")
+    if y.shape[0] != x.shape[0]:
+        raise AetError(1, f"y: {y.shape[0]} classes for {x.shape[0]} rows")
+    if gradient is not None:
+        _kind(gradient, "float32", "gradient")
+        if (gradient.size if isinstance(gradient, np.ndarray) else gradient.numel()) != aet_n_params(h):
+            raise AetError(1, "gradient: as many values as the model has parameters are expected")
     loss, right = C.c_double(), C.c_uint64()
     _check(h, _lib.load().aet_evaluate(h, node, _ptr(x), _ptr(y), x.shape[0], None if dropout is None else C.addressof(dropout),
                                        C.addressof(loss), C.addressof(right), _ptr(gradient), _stream(stream)))

@@ -200,6 +200,24 @@ def test_dense_gradient_agrees_with_differences():
             assert abs((side[0] - side[1]) / (2 * h) - got) <= 0.003 * float(c["dy"].abs().sum()) / n_out + 2.0 ** -13, (name, at)
 
 
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("act", ["relu", "gelu", "silu"])
+def test_activations_and_slopes_at_extreme_values(act, type):
+    """The type's largest and lowest values and zeros of both signs through a 1 x 1 layer of weight 1: finite, and a slope of 0 or 1 far out."""
+    t = lh.TYPES[type]
+    top = torch.finfo(t).max
+    z = torch.tensor([top, -top, 0.0, -0.0, 60.0, -60.0], device="cuda").to(t)[:, None]
+    rows, one = z.shape[0], torch.ones(1, 1, dtype=t, device="cuda")
+    plan = api.aet_dense(1, 1, dtype=t, act=act)
+    y, dx = torch.empty_like(z), torch.empty_like(z)
+    for n in (rows, 1):                                      # the FMA kernel's rows stand for all kernels: one epilogue; a single row has its own
+        api.aet_dense_forward(plan, z[:n], one, None, y[:n], workspace=workspace(plan, n, False))
+    api.aet_dense_backward(plan, z, one, torch.ones_like(z), pre=z, dx=dx, workspace=workspace(plan, rows, True))
+    assert torch.equal(y[:2, 0], torch.stack([z[0, 0], torch.zeros_like(z[0, 0])])) and not y[2:4].any()
+    assert dx[0] == 1 and dx[1] == 0 and float(dx[2]) == float(dx[3]) == {"relu": 0.0, "gelu": 0.5, "silu": 0.5}[act]
+    assert y[4] == z[4] and dx[4] == 1 and abs(float(y[5])) <= 1e-20 and abs(float(dx[5])) <= 1e-20
+
+
 # ---- loss ----------------------------------------------------------------------------------------------------------------
 
 def loss_reference(z, labels, scale, weight):

@@ -141,3 +141,12 @@ def test_binding_refuses_what_does_not_fit():
         api.aet_dense_forward(api.aet_dense(4, 4), x, x, None, x)
     with pytest.raises(api.AetError, match="w:"):
         api.aet_dense_forward(api.aet_dense(3, 4), x, x, None, x)
+
+
+def test_evaluation_binding_refuses_other_types():
+    import numpy as np
+    x, y = np.zeros((4, 3), dtype=np.float32), np.zeros(4, dtype=np.int32)
+    for bad in (lambda: api.aet_evaluate(None, 0, x.astype(np.float64), y), lambda: api.aet_evaluate(None, 0, x, y.astype(np.int64)),
+                lambda: api.aet_evaluate(None, 0, x, y[:3]), lambda: api.aet_predict(None, 0, x), lambda: api.aet_predict(None, 0, x, np.zeros((3, 2), dtype=np.float32))):
+        with pytest.raises(api.AetError):
+            bad()
