@@ -203,6 +203,20 @@ __device__ __forceinline__ void finish4(const Epilogue& e, size_t row, uint32_t 
   finish4<Out>(e, row, col, cols, n, v, r);
 }
 
+// One sum of a product, the bias not in it yet, where neighbouring lanes have neighbouring columns.
+template <class Out>
+__device__ __forceinline__ void finish1(const Epilogue& e, size_t row, uint32_t col, uint32_t cols, float v) {
+  if (e.bias) {
+    float b[4];
+    load4(e.bias_type, e.bias, col, false, 1, b);
+    v += b[0];
+  }
+  if (e.pre) static_cast<Out*>(e.pre)[row * e.ld_pre + col] = from_f32<Out>(v);
+  v = activate<Out>(e.act, v);
+  if (e.drop.q) v = ((uint32_t)(mix64(drop_at(e.drop, row, cols, col)) >> (col % 4 * 16)) & 0xFFFFu) >= e.drop.q ? v * e.drop.scale : 0.f;
+  if (e.residual) v += to_f32(static_cast<const Out*>(e.residual)[row * e.ld_res + col]);
+  static_cast<Out*>(e.out)[row * e.ld_out + col] = from_f32<Out>(v);
+}
 // Four sums of a product, the bias not in them yet.
 template <class Out>
 __device__ __forceinline__ void with_bias(const Product& p, uint32_t row, uint32_t col, float (&v)[4]) {

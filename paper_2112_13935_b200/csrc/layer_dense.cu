@@ -76,7 +76,7 @@ struct Copies {
 };
 
 // What a forward call does and where it keeps what it needs.
-struct Forward { bool few, mma; MmaShape shape; Copy x, w; size_t partial, total; };
+struct Forward { bool few, mma, swapped; MmaShape shape; Copy x, w; size_t partial, total; };
 Forward plan_forward(const Dense& L, size_t rows) {
   const aet_dense_desc& d = L.d;
   Forward f{};
@@ -84,9 +84,10 @@ Forward plan_forward(const Dense& L, size_t rows) {
   if (f.few) return f;
   f.mma = mma_takes(d.dtype, (uint32_t)rows, d.n_out, d.n_in);
   if (!f.mma) return f;
-  f.shape = mma_shape(d.dtype, (uint32_t)rows, d.n_out, d.n_in);
-  f.x = plan_copy(d, rows, d.n_in, d.ld_x, false, f.total);
-  f.w = plan_copy(d, d.n_in, d.n_out, d.ld_w, by_parts(d), f.total);
+  f.swapped = by_parts(d) && rows < d.n_out;        // the smaller operand is the one in parts
+  f.shape = f.swapped ? mma_shape(d.dtype, d.n_out, (uint32_t)rows, d.n_in) : mma_shape(d.dtype, (uint32_t)rows, d.n_out, d.n_in);
+  f.x = plan_copy(d, rows, d.n_in, d.ld_x, f.swapped, f.total);
+  f.w = plan_copy(d, d.n_in, d.n_out, d.ld_w, by_parts(d) && !f.swapped, f.total);
   f.partial = f.total;
   f.total += round_up(mma_partial_floats(f.shape, (uint32_t)rows, d.n_out) * sizeof(float), 256);
   return f;
@@ -160,7 +161,8 @@ cudaError_t dense_forward(const Dense& L, size_t rows, const void* x, const void
   copies.add(f.x, d, x, d.ld_x, rows, d.n_in, ws);
   copies.add(f.w, d, w, d.ld_w, d.n_in, d.n_out, ws);
   if (const cudaError_t e = launch_rows_copies(copies.list, copies.n, s)) return e;
-  return launch_product_mma(MmaProduct{p, operand(f.x, x, ws, false), operand(f.w, w, ws, true), d.dtype, f.shape, reinterpret_cast<float*>(ws + f.partial)}, s);
+  const MmaOperand ox = operand(f.x, x, ws, false), ow = operand(f.w, w, ws, true);
+  return launch_product_mma(MmaProduct{p, f.swapped ? ow : ox, f.swapped ? ox : ow, d.dtype, f.shape, reinterpret_cast<float*>(ws + f.partial), f.swapped}, s);
 }
 
 cudaError_t dense_backward(const Dense& L, size_t rows, const void* x, const void* w, const void* pre, const void* dy, void* dx, void* dw, void* db,

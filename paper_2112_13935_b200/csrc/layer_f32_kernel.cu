@@ -6,6 +6,9 @@
 // store the parts in tensor memory, from where tcgen05.mma reads its A operand.  So A's parts cost neither memory traffic nor shared-memory
 // bandwidth: reading A (16 KB every 768 cycles of six products) and multiplying take about the same time where B has 128 columns.
 //
+// Swapped, C^T = B^T A^T: where A has fewer rows than B columns (few rows through a wide layer) the parts are A's and the weights are read
+// once, as they are (64 x 4,096 x 4,096 25 us; 66 with a pass for the weights' parts).  A lane then has a column of C.
+//
 // One persistent CTA per SM: a thread for TMA, a thread that issues, four warps that take apart (some 230
 // instructions a stage: more warps would leave fewer registers for the sums, which then spill), eight that take sums out.  Tensor cores
 // cut the sums they form: sums of 64 of k (24 additions) leave tensor memory and are added up in registers in fp32.  Against 64 bits the
@@ -47,7 +50,7 @@ __device__ __forceinline__ void mma_a_tmem(uint32_t d, uint32_t a, uint32_t b_lo
                ::"r"(d), "r"(a), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate) : "memory");
 }
 
-template <int BN>
+template <int BN, bool kSwapped>
 __global__ void __launch_bounds__((Ring<BN>::threads), 1) product_f32_kernel(const __grid_constant__ Launch L, const __grid_constant__ CUtensorMap map_a,
                                                                              const __grid_constant__ CUtensorMap map_b) {
   using R = Ring<BN>;
@@ -180,9 +183,22 @@ __global__ void __launch_bounds__((Ring<BN>::threads), 1) product_f32_kernel(con
 #pragma unroll
           for (int i = 0; i < kBlock; ++i) sum[c][i] = CUDART_NAN_F;
         }
-        Ahead<float> ahead;
-        ahead.ask(L, lane, m0, n0 + c * kBlock);
-        store_block<float>(L, t.split, buf, lane, sum[c], ahead, m0, n0 + c * kBlock);
+        if (kSwapped) {       // a lane has a column of C, and its registers the rows: lanes store neighbours as they are
+          const uint32_t col = m0 + lane;
+          if (col < L.p.n) {
+#pragma unroll
+            for (int i = 0; i < kBlock; ++i) {
+              const uint32_t row = n0 + c * kBlock + i;
+              if (row >= L.p.m) break;
+              if (L.splits > 1) L.partial[((size_t)t.split * L.p.m + row) * L.ld_partial + col] = sum[c][i];
+              else finish1<float>(L.p.e, row, col, L.p.n, sum[c][i]);
+            }
+          }
+        } else {
+          Ahead<float> ahead;
+          ahead.ask(L, lane, m0, n0 + c * kBlock);
+          store_block<float>(L, t.split, buf, lane, sum[c], ahead, m0, n0 + c * kBlock);
+        }
       }
     }
   } else {
@@ -232,22 +248,23 @@ __global__ void __launch_bounds__((Ring<BN>::threads), 1) product_f32_kernel(con
   if (warp == 1) tmem_free<1>(tmem, 512);
 }
 
-template <int BN>
+template <int BN, bool kSwapped>
 cudaError_t run(const MmaProduct& m, cudaStream_t s) {
   using R = Ring<BN>;
+  const uint32_t rows = kSwapped ? m.p.n : m.p.m, cols = kSwapped ? m.p.m : m.p.n;     // of the product as the tensor cores see it
   Launch L{};
   L.p = m.p;
   L.a_mn = m.a.mn; L.b_mn = m.b.mn;
   L.splits = m.shape.splits;
   L.partial = m.partial; L.ld_partial = ((size_t)m.p.n + 3) / 4 * 4;
-  L.tiles_m = (m.p.m + 127) / 128;
-  L.tiles_n = (m.p.n + BN - 1) / BN;
+  L.tiles_m = (rows + 127) / 128;
+  L.tiles_n = (cols + BN - 1) / BN;
   L.idesc = (1u << 4) | (1u << 7) | (1u << 10) | (L.b_mn << 16) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
   CUtensorMap ma, mb;
-  cudaError_t e = L.a_mn ? encode(&ma, m.a, kF32, 1, m.p.m, m.p.k, 32, R::bk) : encode(&ma, m.a, kF32, 1, m.p.k, m.p.m, R::bk, 128);
-  if (e == cudaSuccess) e = L.b_mn ? encode(&mb, m.b, kBf16, 3, m.p.n, m.p.k, 64, R::bk) : encode(&mb, m.b, kBf16, 3, m.p.k, m.p.n, R::bk, BN);
+  cudaError_t e = L.a_mn ? encode(&ma, m.a, kF32, 1, rows, m.p.k, 32, R::bk) : encode(&ma, m.a, kF32, 1, m.p.k, rows, R::bk, 128);
+  if (e == cudaSuccess) e = L.b_mn ? encode(&mb, m.b, kBf16, 3, cols, m.p.k, 64, R::bk) : encode(&mb, m.b, kBf16, 3, m.p.k, cols, R::bk, BN);
   if (e != cudaSuccess) return e;
-  const auto kernel = product_f32_kernel<BN>;
+  const auto kernel = product_f32_kernel<BN, kSwapped>;
   e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, R::total);
   if (e != cudaSuccess) return e;
   uint32_t slots = 0;
@@ -263,7 +280,10 @@ cudaError_t run(const MmaProduct& m, cudaStream_t s) {
 }  // namespace
 
 // 64 columns at a time where there are no more (a tile of 128 would multiply zeros half of the time)
-cudaError_t launch_product_f32(const MmaProduct& m, cudaStream_t s) { return m.p.n <= 64 ? run<64>(m, s) : run<128>(m, s); }
+cudaError_t launch_product_f32(const MmaProduct& m, cudaStream_t s) {
+  if (m.swapped) return m.p.m <= 64 ? run<64, true>(m, s) : run<128, true>(m, s);
+  return m.p.n <= 64 ? run<64, false>(m, s) : run<128, false>(m, s);
+}
 
 }  // namespace layer
 }  // namespace aet

@@ -233,8 +233,9 @@ MmaShape mma_shape(uint32_t type, uint32_t m, uint32_t n, uint32_t k) {
   const uint64_t cols = type == kF32 && n <= 64 ? 64 : 128;
   const uint64_t tiles = r.pair ? pairs : ((uint64_t)m + 127) / 128 * ((n + cols - 1) / cols), slots = r.pair ? 74 : 148;
   const uint64_t kbs = ((uint64_t)k + 63) / 64;
-  uint64_t splits = slots / tiles;                       // as many parts as there are SMs left, each with 256 of k and more
-  if (splits > kbs / 4) splits = kbs / 4;
+  uint64_t splits = slots / tiles;                       // as many parts as there are SMs left, each with 256 of k (fp32: 128) and more
+  const uint64_t least = type == kF32 ? 2 : 4;
+  if (splits > kbs / least) splits = kbs / least;
   if (splits > 32) splits = 32;
   r.splits = splits < 2 ? 1 : (uint32_t)splits;
   return r;

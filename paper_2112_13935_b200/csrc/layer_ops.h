@@ -69,6 +69,7 @@ struct MmaProduct {
   uint32_t type;
   MmaShape shape;
   float* partial;    // mma_partial_floats() of workspace
+  uint32_t swapped;  // fp32: a is B^T and b A^T, in parts; `shape` is that of n x m
 };
 bool mma_takes(uint32_t type, uint32_t m, uint32_t n, uint32_t k);   // rather than the FMA kernel
 MmaShape mma_shape(uint32_t type, uint32_t m, uint32_t n, uint32_t k);

@@ -91,7 +91,7 @@ def test_dense_forward_large(rows, n_in, n_out, type):
 
 
 @pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
-@pytest.mark.parametrize("rows,n_in,n_out", [(300, 785, 300), (100, 9000, 130), (2305, 72, 2100)])
+@pytest.mark.parametrize("rows,n_in,n_out", [(300, 785, 300), (100, 9000, 130), (2305, 72, 2100), (9, 5000, 3001), (65, 700, 5002)])
 @pytest.mark.parametrize("over", [dict(pad=1, residual=True, act="silu", pre=True), dict(pad=3, shift=1, rate=0.1, residual=True), dict(pad=8, bias=False, residual=True, in_place=True)])
 def test_dense_forward_large_options(rows, n_in, n_out, type, over):
     check_forward(rows, n_in, n_out, type, **over)
