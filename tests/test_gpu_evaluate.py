@@ -1,4 +1,4 @@
-"""Evaluation of a handle's model against the checker's losses and gradients in 64 bits."""
+"""Evaluation of a handle's model against the oracle's losses and gradients in 64 bits."""
 import numpy as np
 import pytest
 import torch
@@ -29,7 +29,7 @@ CASES = [((784, 10), 0, 0.0, 300), ((784, 10), 0, 1e-3, 1), ((785, 7), 0, 1e-4, 
 
 @pytest.mark.parametrize("dims,precision,l2,n", CASES)
 @pytest.mark.parametrize("where", ["host", "device"])
-def test_evaluation_against_the_checker(dims, precision, l2, n, where):
+def test_evaluation_against_the_oracle(dims, precision, l2, n, where):
     cfg, s, r = session(dims, precision, l2)
     with s:
         s.run(2)
@@ -43,7 +43,7 @@ def test_evaluation_against_the_checker(dims, precision, l2, n, where):
         z = put(np.zeros((n, dims[-1]), dtype=np.float32))
         api.aet_predict(s.h, 1, put(x), z)
         grad, z = (lh.host(v) if where == "device" else v.astype(np.float64) for v in (grad, z))
-        # fp32: sums of up to 785 terms in a few layers, some 1e-6.  bf16: roundings that the checker's 64-bit sums and these fp32 sums take differently
+        # fp32: sums of up to 785 terms in a few layers, some 1e-6.  bf16: roundings that the oracle's 64-bit sums and these fp32 sums take differently
         # (a hidden value by 2^-8 of itself, here and there) and ReLU masks that flip with them
         tol = 1e-5 if precision == 0 else 3e-2
         assert abs(loss - want_loss) <= (1e-6 if precision == 0 else 2e-4) * max(1.0, want_loss)
