@@ -23,25 +23,35 @@ namespace {
 constexpr int kThreads = 256, kNone = 0x7fffffff;
 
 // Exponentials are powers of two: e^(z - m) as 2^(c z - t), one fused multiply-add and one instruction of the special function unit each,
-// with c = log2 e and t = c m; t's own rounding is put right where a sum becomes a loss, so that only z - m enters the error, with 2^-24.
-// A maximum over 2^100 (the type's lowest value as a mask of all the row) takes c = 1 and t = m, since c m may overflow: whatever is not
-// the maximum lies so far below it that its power is 0 either way.
+// with c = log2 e and t = c m rounded.  The maximum's own exponent is then t's rounding, which all the row's sum shares and which is put right
+// where a sum becomes a loss, so that only z - m enters the error, with 2^-24.  That holds while the rounding is small: up to |m| = 2^20 it
+// is 2^-4 at most.  At 1e10 it would be 440, and a row masked with -1e10 had the sum inf.  A maximum further out is subtracted first,
+// 2^((z - m) c), with no rounding of its own and one instruction more; the difference of two fp32 values that matters is exact there.
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 __device__ __forceinline__ float exp2_of(float x) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-struct Base { float c, t; };
-__device__ __forceinline__ bool huge(float top) { return fabsf(top) > 0x1p100f; }
+struct Base { float t; bool far; };
+__device__ __forceinline__ bool far_out(float top) { return fabsf(top) > 0x1p20f && !isinf(top); }
 __device__ __forceinline__ Base base_of(float top) {
-  return isinf(top) ? Base{kLog2e, 0.f} : huge(top) ? Base{1.f, top} : Base{kLog2e, __fmul_rn(top, kLog2e)};
+  const bool far = far_out(top);
+  return Base{isinf(top) ? 0.f : far ? top : __fmul_rn(top, kLog2e), far};
 }
+template <bool kFar> __device__ __forceinline__ float power(float z, float t) { return exp2_of(kFar ? (z - t) * kLog2e : fmaf(z, kLog2e, -t)); }
+// What is done with a row's powers, one way or the other: asked once a row, since a branch in the loops over pieces cost 2 % of long rows.
+template <class F> __device__ __forceinline__ void by_base(const Base& b, const F& f) {
+  if (b.far) f(std::true_type{});
+  else f(std::false_type{});
+}
+// The maximum's own exponent by its base.
+__device__ __forceinline__ float excess(float top) { return far_out(top) || isinf(top) ? 0.f : fmaf(top, kLog2e, -__fmul_rn(top, kLog2e)); }
 // What a sum by the base of maximum `top` is multiplied by to be one by that of a maximum `to` that is not below it.
 __device__ __forceinline__ float rebase(float top, float to) {
-  return exp2_of(huge(top) || huge(to) ? (top - to) * kLog2e : __fmul_rn(top, kLog2e) - __fmul_rn(to, kLog2e));
+  return exp2_of(far_out(top) || far_out(to) || isinf(to) ? (top - to) * kLog2e + (excess(to) - excess(top)) : __fmul_rn(top, kLog2e) - __fmul_rn(to, kLog2e));
 }
-// What a part of a row says: its maximum, the first piece it stands in, and the sum of 2^(c z - t) by the maximum's base.  The sum is NaN
+// What a part of a row says: its maximum, the first piece it stands in, and the sum of powers by the maximum's base.  The sum is NaN
 // where a logit is and only there (a maximum that is infinite counts as zero); a row whose maximum is infinite has no loss: NaN.
 struct Part { float top, sum; int32_t at; };
 // Maximum, sum and minimum over N neighbouring lanes, the same in all of them.
@@ -106,11 +116,11 @@ template <class T> __device__ __forceinline__ float largest(const uint4& v) {
     return fmaxf(f[0], f[1]);
   }
 }
-template <class T> __device__ __forceinline__ float powers(const uint4& v, const Base& b) {
+template <class T, bool kFar> __device__ __forceinline__ float powers(const uint4& v, float t) {
   float f[kV<T>], sum = 0.f;
   unpack<T, kV<T>>(v, f);
 #pragma unroll
-  for (int k = 0; k < kV<T>; ++k) sum += exp2_of(fmaf(f[k], b.c, -b.t));
+  for (int k = 0; k < kV<T>; ++k) sum += power<kFar>(f[k], t);
   return sum;
 }
 
@@ -129,12 +139,12 @@ template <class T> struct Slope {
     whole = ((uintptr_t)g / sizeof(T) + kV<T> - shift) % kV<T> == 0;
   }
 };
-template <class T> __device__ __forceinline__ void write_grad(const Row<T>& r, const uint4& q, int32_t at, const Slope<T>& s, bool whole) {
+template <bool kFar, class T> __device__ __forceinline__ void write_grad(const Row<T>& r, const uint4& q, int32_t at, const Slope<T>& s, bool whole) {
   const int32_t j = at * kV<T> - r.shift;
   float v[kV<T>];
   unpack<T, kV<T>>(q, v);
 #pragma unroll
-  for (int i = 0; i < kV<T>; ++i) v[i] = exp2_of(fmaf(v[i], s.b.c, -s.b.t)) * s.w;
+  for (int i = 0; i < kV<T>; ++i) v[i] = power<kFar>(v[i], s.b.t) * s.w;
   if (whole) {
     __stcs(reinterpret_cast<uint4*>(s.g + j), pack<T, kV<T>>(v));
   } else {
@@ -146,11 +156,11 @@ template <class T> __device__ __forceinline__ void write_grad(const Row<T>& r, c
 // ... at the label, by the thread that has written its piece.
 template <class T> __device__ __forceinline__ int32_t label_piece(const Row<T>& r, int32_t y) { return (uint32_t)y < (uint32_t)r.n ? (y + r.shift) / kV<T> : -1; }
 template <class T> __device__ __forceinline__ void write_label(const Slope<T>& s, float zy) {
-  s.g[s.y] = from_f32<T>(s.f * (exp2_of(fmaf(zy, s.b.c, -s.b.t)) * s.inv - 1.f));
+  s.g[s.y] = from_f32<T>(s.f * ((s.b.far ? power<true>(zy, s.b.t) : power<false>(zy, s.b.t)) * s.inv - 1.f));
 }
 // The loss, and -1 or 0 for a row without a first maximum (a NaN; -inf only); otherwise who holds its piece writes `top`.
 __device__ __forceinline__ void write_loss(const LossLaunch& p, size_t row, const Part& a, float zy) {
-  if (p.loss) p.loss[row] = isinf(a.top) ? CUDART_NAN_F : logf(a.sum) - (huge(a.top) ? 0.f : kLn2 * fmaf(a.top, kLog2e, -__fmul_rn(a.top, kLog2e))) + (a.top - zy);
+  if (p.loss) p.loss[row] = isinf(a.top) ? CUDART_NAN_F : logf(a.sum) - kLn2 * excess(a.top) + (a.top - zy);
   if (p.top && (a.sum != a.sum || a.at == kNone)) p.top[row] = a.sum != a.sum ? -1 : 0;
 }
 template <class T> __device__ __forceinline__ void write_top(const LossLaunch& p, const Row<T>& r, size_t row, const Part& a, const uint4& q, int32_t at) {
@@ -213,8 +223,10 @@ __global__ void __launch_bounds__(kThreads) loss_lanes_kernel(const LossLaunch p
   a.at = p.top ? lanes_min<G>(top == a.top ? at : kNone) : 0;
   a.sum = 0.f;
   const Base b = base_of(a.top);
+  by_base(b, [&](auto far) {
 #pragma unroll
-  for (int i = 0; i < NV; ++i) a.sum += powers<T>(q[i], b);
+    for (int i = 0; i < NV; ++i) a.sum += powers<T, decltype(far)::value>(q[i], b.t);
+  });
   a.sum = lanes_sum<G>(a.sum);
   __syncwarp();      // (the row has been read before its gradient may take its place)
   if (!here) return;
@@ -229,9 +241,11 @@ __global__ void __launch_bounds__(kThreads) loss_lanes_kernel(const LossLaunch p
   }
   if (p.grad) {
     const Slope<T> s(p, row, y, a, r.shift);
+    by_base(s.b, [&](auto far) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (lane + i * G < r.count) write_grad(r, q[i], lane + i * G, s, s.whole && !r.ragged(lane + i * G));
+      for (int i = 0; i < NV; ++i)
+        if (lane + i * G < r.count) write_grad<decltype(far)::value>(r, q[i], lane + i * G, s, s.whole && !r.ragged(lane + i * G));
+    });
     const int32_t at = label_piece(r, y);
     if (at >= 0 && at % G == lane) write_label(s, zy);
   }
@@ -291,8 +305,10 @@ __global__ void __launch_bounds__(THREADS) loss_cluster_kernel(const LossLaunch 
 #pragma unroll
   for (int i = 0; i < THREADS / 32; ++i) a.top = fmaxf(a.top, tops[i]);
   const Base b = base_of(a.top);
+  by_base(b, [&](auto far) {
 #pragma unroll 2
-  for (int32_t c = q0 + tid; c < q1; c += THREADS) sum += powers<T>(piece(c), b);
+    for (int32_t c = q0 + tid; c < q1; c += THREADS) sum += powers<T, decltype(far)::value>(piece(c), b.t);
+  });
   sum = lanes_sum<32>(sum);
   first = p.top ? lanes_min<32>(top == a.top ? first : kNone) : 0;
   if (tid % 32 == 0) sums[tid / 32] = sum, firsts[tid / 32] = first;
@@ -317,18 +333,21 @@ __global__ void __launch_bounds__(THREADS) loss_cluster_kernel(const LossLaunch 
   if (p.top && a.at >= q0 && a.at < q1 && (a.at - q0) % THREADS == tid) write_top(p, r, row, a, piece(a.at), a.at);
   if (!p.grad) return;
   const Slope<T> s(p, row, y, a, r.shift);
-  if (s.whole) {
-    const int32_t i0 = r.ragged(0), i1 = r.count - r.ragged(r.count - 1);     // pieces within [i0, i1) are the row's alone
+  by_base(s.b, [&](auto far) {
+    constexpr bool kFar = decltype(far)::value;
+    if (s.whole) {
+      const int32_t i0 = r.ragged(0), i1 = r.count - r.ragged(r.count - 1);     // pieces within [i0, i1) are the row's alone
 #pragma unroll 2
-    for (int32_t c = q0 + tid; c < q1; c += THREADS)
-      if (c >= i0 && c < i1) write_grad(r, piece(c), c, s, true);
-    for (int32_t e = 0; e < 2; ++e) {
-      const int32_t c = e ? r.count - 1 : 0;
-      if (r.ragged(c) && c >= q0 && c < q1 && (c - q0) % THREADS == tid) write_grad(r, piece(c), c, s, false);
+      for (int32_t c = q0 + tid; c < q1; c += THREADS)
+        if (c >= i0 && c < i1) write_grad<kFar>(r, piece(c), c, s, true);
+      for (int32_t e = 0; e < 2; ++e) {
+        const int32_t c = e ? r.count - 1 : 0;
+        if (r.ragged(c) && c >= q0 && c < q1 && (c - q0) % THREADS == tid) write_grad<kFar>(r, piece(c), c, s, false);
+      }
+    } else {
+      for (int32_t c = q0 + tid; c < q1; c += THREADS) write_grad<kFar>(r, piece(c), c, s, false);
     }
-  } else {
-    for (int32_t c = q0 + tid; c < q1; c += THREADS) write_grad(r, piece(c), c, s, false);
-  }
+  });
   const int32_t at = label_piece(r, y);
   if (at >= q0 && at < q1 && (at - q0) % THREADS == tid) write_label(s, zy);
 }
