@@ -334,7 +334,10 @@ def _row_major(t, dtype, dev, shape, what):
     if t is None:
         return None, 0
     ld = t.stride(0) if shape[0] > 1 and len(t.shape) == 2 else shape[1]
-    return _at(t, dtype, dev, shape, what, ld), ld
+    at = _at(t, dtype, dev, shape, what, ld)
+    if ld < shape[1]:       # (a broadcast tensor's rows are 0 apart, which the library would take for no gaps)
+        raise AetError(1, f"{what}: strides {t.stride()}, expected rows {shape[1]} or more elements apart")
+    return at, ld
 
 
 def aet_dropout_spec(seed: int, client: int = 0, counter: int = 0, rate: float = 0.0):
