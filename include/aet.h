@@ -240,8 +240,8 @@ aet_status aet_get_node_model(aet_handle* h, uint32_t node, float* out, size_t n
 aet_status aet_get_event_log(aet_handle* h, aet_event* out, size_t capacity,
                              size_t* n_events, aet_summary* summary);
 
-/* Logits of `n` rows x [n, dims[0]] by the model of node `node` (as
- * aet_get_node_model has it): [n, classes] fp32, host or device pointers.  Softmax
+/* Logits of `n` rows x [n, aet_n_inputs()] by the model of node `node` (as
+ * aet_get_node_model has it): [n, aet_n_classes()] fp32, host or device pointers.  Softmax
  * regression and ReLU MLPs; precision 1 rounds inputs, weights and hidden
  * activations to bf16 as its rounds do.  Runs on the layer operators below, in
  * chunks of rows whose workspace the handle keeps.  Synchronises `cuda_stream`.
@@ -308,6 +308,11 @@ aet_status aet_set_kernel_timing(aet_handle* h, int enable);
 aet_status aet_get_stats(aet_handle* h, aet_stats* out);
 
 size_t aet_n_params(const aet_handle* h);
+/* Values in a row of the model's inputs, and its classes: the widths of the rows that
+ * aet_load_client_data, aet_predict and aet_evaluate read and of the logits that
+ * aet_predict writes (0 for a null handle). */
+size_t aet_n_inputs(const aet_handle* h);
+size_t aet_n_classes(const aet_handle* h);
 
 /* Text of the most recent error on this handle ("" if none); h may be null for
  * the last aet_create failure of the calling thread. */

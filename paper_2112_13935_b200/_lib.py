@@ -84,6 +84,8 @@ PROTOTYPES = {
     "aet_set_kernel_timing": (C.c_int, [C.c_void_p, C.c_int]),
     "aet_get_stats": (C.c_int, [C.c_void_p, C.POINTER(AetStats)]),
     "aet_n_params": (C.c_size_t, [C.c_void_p]),
+    "aet_n_inputs": (C.c_size_t, [C.c_void_p]),
+    "aet_n_classes": (C.c_size_t, [C.c_void_p]),
     "aet_last_error": (C.c_char_p, [C.c_void_p]),
     "aet_round_no_alloc": (C.c_int, [C.POINTER(AetConfig), C.c_uint32, C.c_uint32, C.c_void_p, C.c_void_p,
                                      C.c_uint32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),

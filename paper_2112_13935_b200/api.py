@@ -113,6 +113,15 @@ def aet_n_params(h) -> int:
     return int(_lib.load().aet_n_params(h))
 
 
+def aet_n_inputs(h) -> int:
+    """Values in a row of the model's inputs."""
+    return int(_lib.load().aet_n_inputs(h))
+
+
+def aet_n_classes(h) -> int:
+    return int(_lib.load().aet_n_classes(h))
+
+
 def aet_get_global_model(h, out=None, stream=None):
     if out is None:
         out = np.empty(aet_n_params(h), dtype=np.float32)
@@ -142,32 +151,37 @@ def _kind(a, kind: str, what: str):
         raise AetError(1, f"{what}: {a.dtype}, expected {kind}")
 
 
+def _rows(a, kind: str, n: int, width: int, what: str):
+    """Held to its type and size, n rows of `width` values: the library gets an address and reads or writes that much behind it."""
+    _kind(a, kind, what)
+    if a.shape[0] != n or (a.size if isinstance(a, np.ndarray) else a.numel()) != n * width:
+        raise AetError(1, f"{what}: {tuple(a.shape)}, expected {n} rows of {width}")
+
+
 def aet_predict(h, node: int, x, logits=None, classes=None, stream=None):
     """Logits [n, classes] of a node's model for the rows of x; host or device arrays (without `logits` a numpy array of `classes` columns)."""
     if logits is None:
         if classes is None:
             raise AetError(1, "either logits or classes is needed")
         logits = np.empty((x.shape[0], classes), dtype=np.float32)
-    _kind(x, "float32", "x")
-    _kind(logits, "float32", "logits")
-    if logits.shape[0] != x.shape[0]:
-        raise AetError(1, f"logits: {logits.shape[0]} rows for {x.shape[0]}")
-    _check(h, _lib.load().aet_predict(h, node, _ptr(x), x.shape[0], _ptr(logits), _stream(stream)))
+    n = x.shape[0]
+    _rows(x, "float32", n, aet_n_inputs(h), "x")
+    _rows(logits, "float32", n, aet_n_classes(h), "logits")
+    _check(h, _lib.load().aet_predict(h, node, _ptr(x), n, _ptr(logits), _stream(stream)))
     return logits
 
 
 def aet_evaluate(h, node: int, x, y, dropout=None, gradient=None, stream=None):
     """(loss, rows the model gets right) of a node's model on rows x with classes y; gradient: where the loss's gradient goes."""
-    _kind(x, "float32", "x")
-    _kind(y, "int32", "y")
-    if y.shape[0] != x.shape[0]:
-        raise AetError(1, f"y: {y.shape[0]} classes for {x.shape[0]} rows")
+    n = x.shape[0]
+    _rows(x, "float32", n, aet_n_inputs(h), "x")
+    _rows(y, "int32", n, 1, "y")
     if gradient is not None:
         _kind(gradient, "float32", "gradient")
         if (gradient.size if isinstance(gradient, np.ndarray) else gradient.numel()) != aet_n_params(h):
             raise AetError(1, "gradient: as many values as the model has parameters are expected")
     loss, right = C.c_double(), C.c_uint64()
-    _check(h, _lib.load().aet_evaluate(h, node, _ptr(x), _ptr(y), x.shape[0], None if dropout is None else C.addressof(dropout),
+    _check(h, _lib.load().aet_evaluate(h, node, _ptr(x), _ptr(y), n, None if dropout is None else C.addressof(dropout),
                                        C.addressof(loss), C.addressof(right), _ptr(gradient), _stream(stream)))
     return float(loss.value), int(right.value)
 

@@ -1156,6 +1156,12 @@ aet_status aet_get_stats(aet_handle* h, aet_stats* out) {
 }
 
 size_t aet_n_params(const aet_handle* h) { return h ? h->P : 0; }
+size_t aet_n_inputs(const aet_handle* h) {
+  if (!h) return 0;
+  const aet_config& c = h->cfg;
+  return c.model == 2 ? (size_t)c.dims[0] * c.dims[0] * c.dims[1] : c.dims[0];
+}
+size_t aet_n_classes(const aet_handle* h) { return h ? h->cfg.dims[h->cfg.n_layers] : 0; }
 
 const char* aet_last_error(const aet_handle* h) { return h ? h->err.c_str() : g_create_error.c_str(); }
 

@@ -138,3 +138,24 @@ def test_evaluation_refusals():
         with pytest.raises(api.AetError) as e:
             s.evaluate(np.zeros((4, 784), dtype=np.float32), np.zeros(4, dtype=np.int32))
         assert e.value.status == 2
+
+
+def test_evaluation_of_rows_that_do_not_fit_the_model():
+    cfg, s, r = session((784, 10))
+    x, y = rows_of(r, 8, (784, 10))
+    with s:
+        assert (api.aet_n_inputs(s.h), api.aet_n_classes(s.h), api.aet_n_params(s.h)) == (784, 10, 7850)
+        for bad in (x[:, :783].copy(), np.zeros((8, 785), dtype=np.float32), torch.zeros(8, 783, device="cuda")):
+            for call in (lambda: s.evaluate(bad, y), lambda: s.predict(bad)):
+                with pytest.raises(api.AetError, match="x:") as e:
+                    call()
+                assert e.value.status == 1
+        for classes in (9, 11):
+            with pytest.raises(api.AetError, match="logits:"):
+                api.aet_predict(s.h, 0, x, classes=classes)
+            with pytest.raises(api.AetError, match="logits:"):
+                api.aet_predict(s.h, 0, x, torch.zeros(8, classes, device="cuda"))
+        assert s.predict(x).shape == (8, 10)
+    conv = workloads.get_config("cfg7", n_clients=1)
+    with api.Session(conv, [], None) as s:
+        assert (api.aet_n_inputs(s.h), api.aet_n_classes(s.h)) == (784, 10)

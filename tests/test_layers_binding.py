@@ -1,8 +1,11 @@
 """What the binding of the layer operators and of the evaluation refuses before it asks the library (no GPU needed)."""
+import types
+
+import numpy as np
 import pytest
 import torch
 
-from paper_2112_13935_b200 import api
+from paper_2112_13935_b200 import _lib, api
 
 SPEC = api.aet_dropout_spec(1, rate=0.5)
 
@@ -38,3 +41,42 @@ def test_one_row_and_one_column_may_have_any_stride():
                  lambda: api.aet_cross_entropy(one_column, torch.zeros(6, dtype=torch.int32))):
         with pytest.raises(api.AetError, match="current CUDA device"):
             call()
+
+
+@pytest.fixture
+def library(monkeypatch):
+    """A library that has a model of 12 inputs, 5 classes and 65 parameters and answers every call."""
+    calls = []
+    fake = types.SimpleNamespace(aet_n_inputs=lambda h: 12, aet_n_classes=lambda h: 5, aet_n_params=lambda h: 65,
+                                 aet_predict=lambda *a: calls.append(a) or 0, aet_evaluate=lambda *a: calls.append(a) or 0)
+    monkeypatch.setattr(_lib, "load", lambda: fake)
+    return calls
+
+
+@pytest.mark.parametrize("make", [np.zeros, torch.zeros], ids=["numpy", "torch"])
+def test_evaluation_holds_its_arrays_to_the_model(library, make):
+    f32, i32 = (np.float32, np.int32) if make is np.zeros else (torch.float32, torch.int32)
+    x, y, z = make((4, 12), dtype=f32), make(4, dtype=i32), make((4, 5), dtype=f32)
+    for bad in (make((4, 11), dtype=f32), make((4, 13), dtype=f32), make((48,), dtype=f32), make((4, 12, 2), dtype=f32)):
+        with pytest.raises(api.AetError, match="x:"):
+            api.aet_predict(None, 0, bad, z, stream=0)
+        with pytest.raises(api.AetError, match="x:"):
+            api.aet_evaluate(None, 0, bad, y, stream=0)
+    for bad in (make((4, 4), dtype=f32), make((4, 6), dtype=f32), make((20,), dtype=f32), make((3, 5), dtype=f32)):
+        with pytest.raises(api.AetError, match="logits:"):
+            api.aet_predict(None, 0, x, bad, stream=0)
+    for classes in (4, 6):
+        with pytest.raises(api.AetError, match="logits:"):
+            api.aet_predict(None, 0, x, classes=classes, stream=0)
+    for bad in (make(3, dtype=i32), make((4, 2), dtype=i32)):
+        with pytest.raises(api.AetError, match="y:"):
+            api.aet_evaluate(None, 0, x, bad, stream=0)
+    assert not library
+    api.aet_predict(None, 0, x, z, stream=0)
+    assert api.aet_predict(None, 0, x, classes=5, stream=0).shape == (4, 5)
+    api.aet_evaluate(None, 0, x.reshape(4, 3, 4), y, stream=0)          # (pictures lie as their rows do)
+    assert [c[3] for c in library[:2]] == [4, 4] and library[2][4] == 4
+
+
+def test_widths_of_no_handle():
+    assert api.aet_n_inputs(None) == api.aet_n_classes(None) == 0
