@@ -95,8 +95,22 @@ def aet_set_global_model(h, w0, stream=None):
                                                _stream(stream)))
 
 
+def _kind(a, kind: str, what: str):
+    if str(a.dtype).rsplit(".", 1)[-1] != kind:
+        raise AetError(1, f"{what}: {a.dtype}, expected {kind}")
+
+
+def _rows(a, kind: str, n: int, width: int, what: str):
+    """Held to its type and size, n rows of `width` values: the library gets an address and reads or writes that much behind it."""
+    _kind(a, kind, what)
+    if a.shape[0] != n or (a.size if isinstance(a, np.ndarray) else a.numel()) != n * width:
+        raise AetError(1, f"{what}: {tuple(a.shape)}, expected {n} rows of {width}")
+
+
 def aet_load_client_data(h, client: int, x, y, stream=None):
     n = x.shape[0]
+    _rows(x, "float32", n, aet_n_inputs(h), "x")
+    _rows(y, "int32", n, 1, "y")
     _check(h, _lib.load().aet_load_client_data(h, client, _ptr(x), _ptr(y), n, _stream(stream)))
 
 
@@ -144,18 +158,6 @@ def aet_get_update_sum(h, seq: int, out=None, stream=None):
     n = out.size if isinstance(out, np.ndarray) else out.numel()
     _check(h, _lib.load().aet_get_update_sum(h, seq, _ptr(out), n, _stream(stream)))
     return out
-
-
-def _kind(a, kind: str, what: str):
-    if str(a.dtype).rsplit(".", 1)[-1] != kind:
-        raise AetError(1, f"{what}: {a.dtype}, expected {kind}")
-
-
-def _rows(a, kind: str, n: int, width: int, what: str):
-    """Held to its type and size, n rows of `width` values: the library gets an address and reads or writes that much behind it."""
-    _kind(a, kind, what)
-    if a.shape[0] != n or (a.size if isinstance(a, np.ndarray) else a.numel()) != n * width:
-        raise AetError(1, f"{what}: {tuple(a.shape)}, expected {n} rows of {width}")
 
 
 def aet_predict(h, node: int, x, logits=None, classes=None, stream=None):

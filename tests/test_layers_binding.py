@@ -48,7 +48,8 @@ def library(monkeypatch):
     """A library that has a model of 12 inputs, 5 classes and 65 parameters and answers every call."""
     calls = []
     fake = types.SimpleNamespace(aet_n_inputs=lambda h: 12, aet_n_classes=lambda h: 5, aet_n_params=lambda h: 65,
-                                 aet_predict=lambda *a: calls.append(a) or 0, aet_evaluate=lambda *a: calls.append(a) or 0)
+                                 aet_predict=lambda *a: calls.append(a) or 0, aet_evaluate=lambda *a: calls.append(a) or 0,
+                                 aet_load_client_data=lambda *a: calls.append(a) or 0)
     monkeypatch.setattr(_lib, "load", lambda: fake)
     return calls
 
@@ -76,6 +77,20 @@ def test_evaluation_holds_its_arrays_to_the_model(library, make):
     assert api.aet_predict(None, 0, x, classes=5, stream=0).shape == (4, 5)
     api.aet_evaluate(None, 0, x.reshape(4, 3, 4), y, stream=0)          # (pictures lie as their rows do)
     assert [c[3] for c in library[:2]] == [4, 4] and library[2][4] == 4
+
+
+def test_client_data_is_held_to_the_model(library):
+    x, y = np.zeros((4, 12), dtype=np.float32), np.zeros(4, dtype=np.int32)
+    for bad in (x[:, :11].copy(), np.zeros((4, 13), dtype=np.float32), x.astype(np.float64), np.zeros(48, dtype=np.float32)):
+        with pytest.raises(api.AetError, match="x:"):
+            api.aet_load_client_data(None, 0, bad, y, stream=0)
+    for bad in (y[:3], y.astype(np.int64), np.zeros((4, 2), dtype=np.int32)):
+        with pytest.raises(api.AetError, match="y:"):
+            api.aet_load_client_data(None, 0, x, bad, stream=0)
+    assert not library
+    api.aet_load_client_data(None, 0, x.reshape(4, 3, 2, 2), y, stream=0)
+    api.aet_load_client_data(None, 0, torch.from_numpy(x), torch.from_numpy(y), stream=0)
+    assert [c[4] for c in library] == [4, 4]
 
 
 def test_widths_of_no_handle():
