@@ -100,9 +100,17 @@ def _kind(a, kind: str, what: str):
         raise AetError(1, f"{what}: {a.dtype}, expected {kind}")
 
 
+def _u32(v: int, what: str) -> int:
+    """Held to what the library's 32-bit arguments can say (ctypes would cut it off)."""
+    if not 0 <= v < 1 << 32:
+        raise AetError(1, f"{what}: {v} is not a number of 32 bits")
+    return v
+
+
 def _rows(a, kind: str, n: int, width: int, what: str):
     """Held to its type and size, n rows of `width` values: the library gets an address and reads or writes that much behind it."""
     _kind(a, kind, what)
+    _u32(n, "rows")
     if a.shape[0] != n or (a.size if isinstance(a, np.ndarray) else a.numel()) != n * width:
         raise AetError(1, f"{what}: {tuple(a.shape)}, expected {n} rows of {width}")
 
@@ -169,7 +177,7 @@ def aet_predict(h, node: int, x, logits=None, classes=None, stream=None):
     n = x.shape[0]
     _rows(x, "float32", n, aet_n_inputs(h), "x")
     _rows(logits, "float32", n, aet_n_classes(h), "logits")
-    _check(h, _lib.load().aet_predict(h, node, _ptr(x), n, _ptr(logits), _stream(stream)))
+    _check(h, _lib.load().aet_predict(h, _u32(node, "node"), _ptr(x), n, _ptr(logits), _stream(stream)))
     return logits
 
 
@@ -183,7 +191,7 @@ def aet_evaluate(h, node: int, x, y, dropout=None, gradient=None, stream=None):
         if (gradient.size if isinstance(gradient, np.ndarray) else gradient.numel()) != aet_n_params(h):
             raise AetError(1, "gradient: as many values as the model has parameters are expected")
     loss, right = C.c_double(), C.c_uint64()
-    _check(h, _lib.load().aet_evaluate(h, node, _ptr(x), _ptr(y), n, None if dropout is None else C.addressof(dropout),
+    _check(h, _lib.load().aet_evaluate(h, _u32(node, "node"), _ptr(x), _ptr(y), n, None if dropout is None else C.addressof(dropout),
                                        C.addressof(loss), C.addressof(right), _ptr(gradient), _stream(stream)))
     return float(loss.value), int(right.value)
 
@@ -357,7 +365,7 @@ def _row_major(t, dtype, dev, shape, what):
 
 
 def aet_dropout_spec(seed: int, client: int = 0, counter: int = 0, rate: float = 0.0):
-    return _lib.AetDropoutSpec(seed=seed, client=client, counter=counter, rate=rate)
+    return _lib.AetDropoutSpec(seed=seed, client=_u32(client, "client"), counter=counter, rate=rate)
 
 
 def aet_dropout(drop, x, y, residual=None, stream=None):
@@ -368,7 +376,7 @@ def aet_dropout(drop, x, y, residual=None, stream=None):
     px, ld_x = _row_major(x, dtype, dev, shape, "x")
     pr, ld_r = _row_major(residual, dtype, dev, shape, "residual")
     py, ld_y = _row_major(y, dtype, dev, shape, "y")
-    _check(None, _lib.load().aet_dropout(_dtype(dtype), shape[0], shape[1], C.addressof(drop), px, ld_x, pr, ld_r, py, ld_y, _stream_of(dev, x, stream)))
+    _check(None, _lib.load().aet_dropout(_dtype(dtype), shape[0], _u32(shape[1], "columns"), C.addressof(drop), px, ld_x, pr, ld_r, py, ld_y, _stream_of(dev, x, stream)))
 
 
 def aet_cross_entropy(logits, labels, loss=None, dlogits=None, top=None, weight=None, scale: float = 1.0, stream=None):
@@ -381,7 +389,7 @@ def aet_cross_entropy(logits, labels, loss=None, dlogits=None, top=None, weight=
     pz, ld_z = _row_major(logits, dtype, dev, shape, "logits")
     pg, ld_g = _row_major(dlogits, dtype, dev, shape, "dlogits")
     _check(None, _lib.load().aet_cross_entropy(
-        _dtype(dtype), shape[0], shape[1], pz, ld_z, _at(labels, torch.int32, dev, one, "labels", None),
+        _dtype(dtype), shape[0], _u32(shape[1], "classes"), pz, ld_z, _at(labels, torch.int32, dev, one, "labels", None),
         _at(weight, torch.float32, dev, one, "weight", None), scale, _at(loss, torch.float32, dev, one, "loss", None), pg, ld_g,
         _at(top, torch.int32, dev, one, "top", None), _stream_of(dev, logits, stream)))
 
@@ -394,7 +402,7 @@ def aet_dense(n_in: int, n_out: int, dtype=None, act: str = "none", dropout=None
     d.dtype = 0 if dtype is None else _dtype(dtype)
     if act not in ACTS:
         raise AetError(1, f"activation {act!r} is not one of {', '.join(ACTS)}")
-    d.act, d.n_in, d.n_out, d.flags = ACTS[act], n_in, n_out, flags
+    d.act, d.n_in, d.n_out, d.flags = ACTS[act], _u32(n_in, "n_in"), _u32(n_out, "n_out"), _u32(flags, "flags")
     d.ld_x = d.ld_dx = ld_in or n_in
     d.ld_w = d.ld_dw = ld_w or n_out
     d.ld_y = d.ld_residual = d.ld_pre = d.ld_dy = ld_out or n_out

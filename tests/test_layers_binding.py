@@ -95,3 +95,22 @@ def test_client_data_is_held_to_the_model(library):
 
 def test_widths_of_no_handle():
     assert api.aet_n_inputs(None) == api.aet_n_classes(None) == 0
+
+
+def test_numbers_past_32_bits_are_refused(library, monkeypatch):
+    """... where the library's argument has 32: they would arrive cut off, as a call on fewer columns or on another client."""
+    monkeypatch.setattr(api, "_stream_of", lambda dev, t, stream: 0)
+    fake = _lib.load()
+    fake.aet_dropout = fake.aet_cross_entropy = lambda *a: library.append(a) or 0
+    wide = torch.empty(1, 2 ** 32 + 5, device="meta")
+    labels = torch.empty(1, dtype=torch.int32, device="meta")
+    many = types.SimpleNamespace(dtype="float32", shape=(2 ** 32 + 1, 12), numel=lambda: (2 ** 32 + 1) * 12)
+    few, y = np.zeros((4, 12), dtype=np.float32), np.zeros(4, dtype=np.int32)
+    for call in (lambda: api.aet_dropout(SPEC, wide, wide), lambda: api.aet_cross_entropy(wide, labels), lambda: api.aet_dense(2 ** 32 + 8, 4),
+                 lambda: api.aet_dense(8, 2 ** 32), lambda: api.aet_dense(8, 4, flags=2 ** 32), lambda: api.aet_dropout_spec(1, client=2 ** 32),
+                 lambda: api.aet_predict(None, 0, many, np.zeros((4, 5), dtype=np.float32), stream=0), lambda: api.aet_evaluate(None, 2 ** 32, few, y, stream=0),
+                 lambda: api.aet_predict(None, 2 ** 32, few, classes=5, stream=0)):
+        with pytest.raises(api.AetError, match="32 bits") as e:
+            call()
+        assert e.value.status == 1
+    assert not library
