@@ -168,6 +168,15 @@ def aet_get_update_sum(h, seq: int, out=None, stream=None):
     return out
 
 
+def _here(a, what: str):
+    """An array of the host or of the current device: the evaluation's kernels read and write a device array where it is."""
+    if isinstance(a, np.ndarray) or not a.is_cuda:
+        return
+    import torch
+    if a.get_device() != torch.cuda.current_device():
+        raise AetError(1, f"{what} has to be on the host or on the current CUDA device, not on {a.device}")
+
+
 def aet_predict(h, node: int, x, logits=None, classes=None, stream=None):
     """Logits [n, classes] of a node's model for the rows of x; host or device arrays (without `logits` a numpy array of `classes` columns)."""
     if logits is None:
@@ -177,6 +186,8 @@ def aet_predict(h, node: int, x, logits=None, classes=None, stream=None):
     n = x.shape[0]
     _rows(x, "float32", n, aet_n_inputs(h), "x")
     _rows(logits, "float32", n, aet_n_classes(h), "logits")
+    _here(x, "x")
+    _here(logits, "logits")
     _check(h, _lib.load().aet_predict(h, _u32(node, "node"), _ptr(x), n, _ptr(logits), _stream(stream)))
     return logits
 
@@ -186,6 +197,8 @@ def aet_evaluate(h, node: int, x, y, dropout=None, gradient=None, stream=None):
     n = x.shape[0]
     _rows(x, "float32", n, aet_n_inputs(h), "x")
     _rows(y, "int32", n, 1, "y")
+    _here(x, "x")
+    _here(y, "y")
     if gradient is not None:
         _kind(gradient, "float32", "gradient")
         if (gradient.size if isinstance(gradient, np.ndarray) else gradient.numel()) != aet_n_params(h):

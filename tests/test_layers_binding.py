@@ -114,3 +114,20 @@ def test_numbers_past_32_bits_are_refused(library, monkeypatch):
             call()
         assert e.value.status == 1
     assert not library
+
+
+def test_evaluation_refuses_arrays_of_another_device(library, monkeypatch):
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+
+    def there(dtype, *shape, device=1):
+        return types.SimpleNamespace(dtype=dtype, shape=shape, numel=lambda: int(np.prod(shape)), is_cuda=True, get_device=lambda: device, device=f"cuda:{device}",
+                                     is_contiguous=lambda: True, data_ptr=lambda: 1 << 20)
+
+    x, y, z = np.zeros((4, 12), dtype=np.float32), np.zeros(4, dtype=np.int32), np.zeros((4, 5), dtype=np.float32)
+    for call in (lambda: api.aet_predict(None, 0, there("float32", 4, 12), z, stream=0), lambda: api.aet_predict(None, 0, x, there("float32", 4, 5), stream=0),
+                 lambda: api.aet_evaluate(None, 0, there("float32", 4, 12), y, stream=0), lambda: api.aet_evaluate(None, 0, x, there("int32", 4), stream=0)):
+        with pytest.raises(api.AetError, match="current CUDA device"):
+            call()
+    assert not library
+    api.aet_predict(None, 0, there("float32", 4, 12, device=0), there("float32", 4, 5, device=0), stream=0)
+    assert len(library) == 1
