@@ -441,6 +441,16 @@ aet_status aet_dense_forward(const aet_dense_desc* d, size_t rows, const void* x
                              const void* bias, const void* residual, void* y, void* pre, void* workspace,
                              size_t workspace_bytes, void* cuda_stream);
 
+/* Failure-detection aid: aet_dense_forward of a product on the tensor cores (without
+ * bias, residual and pre), as if the copies of the first CTA, or pair of CTAs, never
+ * came from its `stages`-th stage (0 on; 64 of n_in, fp32: 32) on.  Every wait gives up
+ * after wait_us microseconds (1 .. 10^6) and some more.  The tiles that were not summed
+ * are NaN, or what the epilogue makes of one, all others as ever, and the CUDA context
+ * stays usable.  AET_ERR_CONFIG where the call takes other kernels. */
+aet_status aet_debug_dense_lost_copies(const aet_dense_desc* d, size_t rows, const void* x, const void* w,
+                                       void* y, void* workspace, size_t workspace_bytes, uint32_t stages,
+                                       uint32_t wait_us, void* cuda_stream);
+
 /* Gradient: dz = dropout(dy) act'(pre), dx = dz W^T, dW = x^T dz, db = sum of dz over
  * the rows.  dx, dw, db may be null, x if dw is, w if dx is, pre if act is
  * AET_ACT_NONE.  The residual's gradient is dy itself.  Large products take dz

@@ -98,6 +98,7 @@ PROTOTYPES = {
                                     C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]),
     "aet_dense_workspace": (C.c_int, [C.c_void_p, C.c_size_t, C.c_int, C.c_void_p]),
     "aet_dense_forward": (C.c_int, [C.c_void_p, C.c_size_t] + [C.c_void_p] * 7 + [C.c_size_t, C.c_void_p]),
+    "aet_debug_dense_lost_copies": (C.c_int, [C.c_void_p, C.c_size_t] + [C.c_void_p] * 4 + [C.c_size_t, C.c_uint32, C.c_uint32, C.c_void_p]),
     "aet_dense_backward": (C.c_int, [C.c_void_p, C.c_size_t] + [C.c_void_p] * 8 + [C.c_size_t, C.c_void_p]),
     "aet_schedule_only": (C.c_int, [C.POINTER(AetConfig), C.c_uint32, C.POINTER(AetEvent), C.c_size_t,
                                     C.POINTER(C.c_size_t), C.POINTER(AetSummary)]),

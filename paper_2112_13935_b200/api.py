@@ -461,6 +461,15 @@ def aet_dense_forward(d, x, w, bias, y, residual=None, pre=None, workspace=None,
         _stream_of(dev, x, stream)))
 
 
+def aet_debug_dense_lost_copies(d, x, w, y, workspace, stages: int, wait_us: int, stream=None):
+    """y = dropout(act(x w)) on the tensor cores as if the first CTA's copies from stage `stages` on never came."""
+    rows, t, dev = _rows_of(d, x, d.n_in, "x")
+    ws, size = _space(workspace, dev)
+    _check(None, _lib.load().aet_debug_dense_lost_copies(
+        C.addressof(d), rows, _at(x, t, dev, (rows, d.n_in), "x", d.ld_x), _at(w, t, dev, (d.n_in, d.n_out), "w", d.ld_w),
+        _at(y, t, dev, (rows, d.n_out), "y", d.ld_y), ws, size, _u32(stages, "stages"), _u32(wait_us, "wait_us"), _stream_of(dev, x, stream)))
+
+
 def aet_dense_backward(d, x, w, dy, pre=None, dx=None, dw=None, db=None, workspace=None, stream=None):
     """dx, dw and db (any of them None) of the layer from dy."""
     n_in, n_out = d.n_in, d.n_out

@@ -84,13 +84,15 @@ extern "C" aet_status aet_dense_workspace(const aet_dense_desc* desc, size_t row
   return AET_OK;
 }
 
-extern "C" aet_status aet_dense_forward(const aet_dense_desc* desc, size_t rows, const void* x, const void* w, const void* bias,
-                                        const void* residual, void* y, void* pre, void* workspace, size_t workspace_bytes,
-                                        void* cuda_stream) {
+namespace {
+
+aet_status forward(const aet_dense_desc* desc, size_t rows, const void* x, const void* w, const void* bias, const void* residual, void* y, void* pre,
+                   void* workspace, size_t workspace_bytes, void* cuda_stream, const Waits* played) {
   Dense L;
   if (const char* why = read_dense(desc, L)) return arg(why);
   const aet_dense_desc& d = L.d;
   if (rows > kMostRows) return arg("rows are up to 2^31 - 1");
+  if (played && !dense_forward_waits(L, rows)) return fail(AET_ERR_CONFIG, "lost copies can be played for products on the tensor cores only");
   if (!rows) return AET_OK;
   if (!x || !w || !y) return arg("null argument");
   for (const void* p : {x, w, bias, residual, (const void*)y, (const void*)pre})
@@ -98,7 +100,24 @@ extern "C" aet_status aet_dense_forward(const aet_dense_desc* desc, size_t rows,
   if (!(d.flags & AET_DENSE_ANY_ADDRESS) && (off_16(x) || off_16(w)))
     return arg("x and w have to start on a 16-byte boundary without AET_DENSE_ANY_ADDRESS");
   if (no_space(workspace, workspace_bytes, dense_space(L, rows, false))) return arg(kNoSpace);
-  return done(dense_forward(L, rows, x, w, bias, residual, y, pre, workspace, (cudaStream_t)cuda_stream));
+  return done(dense_forward(L, rows, x, w, bias, residual, y, pre, workspace, (cudaStream_t)cuda_stream, played ? *played : Waits()));
+}
+
+}  // namespace
+
+extern "C" aet_status aet_dense_forward(const aet_dense_desc* desc, size_t rows, const void* x, const void* w, const void* bias,
+                                        const void* residual, void* y, void* pre, void* workspace, size_t workspace_bytes,
+                                        void* cuda_stream) {
+  return forward(desc, rows, x, w, bias, residual, y, pre, workspace, workspace_bytes, cuda_stream, nullptr);
+}
+
+extern "C" aet_status aet_debug_dense_lost_copies(const aet_dense_desc* desc, size_t rows, const void* x, const void* w, void* y, void* workspace,
+                                                  size_t workspace_bytes, uint32_t stages, uint32_t wait_us, void* cuda_stream) {
+  if (!wait_us || wait_us > 1000000) return arg("wait_us is 1 to 10^6");
+  Waits played;
+  played.ns = wait_us * 1000ull;
+  played.stages = stages;
+  return forward(desc, rows, x, w, nullptr, nullptr, y, nullptr, workspace, workspace_bytes, cuda_stream, &played);
 }
 
 extern "C" aet_status aet_dense_backward(const aet_dense_desc* desc, size_t rows, const void* x, const void* w, const void* pre, const void* dy,

@@ -138,7 +138,7 @@ size_t dense_space(const Dense& L, size_t rows, bool backward) {
 }
 
 cudaError_t dense_forward(const Dense& L, size_t rows, const void* x, const void* w, const void* bias, const void* residual, void* y, void* pre,
-                          void* workspace, cudaStream_t s) {
+                          void* workspace, cudaStream_t s, const Waits& waits) {
   const aet_dense_desc& d = L.d;
   const uint32_t out = L.wide ? kF32 : d.dtype;
   const Forward f = plan_forward(L, rows);
@@ -162,8 +162,9 @@ cudaError_t dense_forward(const Dense& L, size_t rows, const void* x, const void
   copies.add(f.w, d, w, d.ld_w, d.n_in, d.n_out, ws);
   if (const cudaError_t e = launch_rows_copies(copies.list, copies.n, s)) return e;
   const MmaOperand ox = operand(f.x, x, ws, false), ow = operand(f.w, w, ws, true);
-  return launch_product_mma(MmaProduct{p, f.swapped ? ow : ox, f.swapped ? ox : ow, d.dtype, f.shape, reinterpret_cast<float*>(ws + f.partial), f.swapped}, s);
+  return launch_product_mma(MmaProduct{p, f.swapped ? ow : ox, f.swapped ? ox : ow, d.dtype, f.shape, reinterpret_cast<float*>(ws + f.partial), f.swapped, waits}, s);
 }
+bool dense_forward_waits(const Dense& L, size_t rows) { return rows && plan_forward(L, rows).mma; }
 
 cudaError_t dense_backward(const Dense& L, size_t rows, const void* x, const void* w, const void* pre, const void* dy, void* dx, void* dw, void* db,
                            void* workspace, cudaStream_t s) {

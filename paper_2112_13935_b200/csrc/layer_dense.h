@@ -18,7 +18,8 @@ const char* read_dense(const aet_dense_desc* in, Dense& out);        // null if 
 // Workspace, and the calls on checked arguments with that much of it (from a 256-byte boundary on).
 size_t dense_space(const Dense& L, size_t rows, bool backward);
 cudaError_t dense_forward(const Dense& L, size_t rows, const void* x, const void* w, const void* bias, const void* residual, void* y, void* pre,
-                          void* workspace, cudaStream_t s);
+                          void* workspace, cudaStream_t s, const Waits& waits = Waits());
+bool dense_forward_waits(const Dense& L, size_t rows);               // on barriers, which may give up: on the tensor cores
 cudaError_t dense_backward(const Dense& L, size_t rows, const void* x, const void* w, const void* pre, const void* dy, void* dx, void* dw, void* db,
                            void* workspace, cudaStream_t s);
 

@@ -60,7 +60,9 @@ __global__ void __launch_bounds__((Ring<BN>::threads), 1) product_f32_kernel(con
   float4* trans = reinterpret_cast<float4*>(sm + R::stages * R::stage);
   const uint32_t bars = base + R::stages * R::stage + R::trans;
   const uint32_t full = bars, empty = bars + 8 * R::stages, apart = bars + 16 * R::stages, acc_full = bars + 24 * R::stages, acc_empty = acc_full + 16,
-                 slot = acc_empty + 16;
+                 slot = acc_empty + 16, drained = slot + 8;
+  volatile uint32_t* gave_up = reinterpret_cast<uint32_t*>(sm + (drained + 8 - base));
+  const unsigned long long ns = L.waits.ns;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t kbs = (L.p.k + R::bk - 1) / R::bk, items = L.tiles_m * L.tiles_n * L.splits;
 
@@ -74,6 +76,8 @@ __global__ void __launch_bounds__((Ring<BN>::threads), 1) product_f32_kernel(con
       bar_init(acc_full + 8 * b, 1);
       bar_init(acc_empty + 8 * b, R::epi_warps);
     }
+    bar_init(drained, 1);
+    *gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) tmem_alloc<1>(slot, 512);
@@ -91,7 +95,7 @@ __global__ void __launch_bounds__((Ring<BN>::threads), 1) product_f32_kernel(con
         const int m0 = (int)(t.m * 128), n0 = (int)(t.n * BN);
         for (uint32_t kb = t.kb0; kb < t.kb1; ++kb, ++it) {
           const uint32_t s = it % R::stages, bar = full + 8 * s, a = base + s * R::stage, b = a + R::a_bytes;
-          ok = bar_wait(empty + 8 * s, (it / R::stages & 1) ^ 1);
+          ok = bar_wait(empty + 8 * s, (it / R::stages & 1) ^ 1, ns) && (blockIdx.x || it < L.waits.stages);
           if (!ok) break;
           bar_expect(bar, R::stage);
           const int k0 = (int)(kb * R::bk);
@@ -109,8 +113,10 @@ __global__ void __launch_bounds__((Ring<BN>::threads), 1) product_f32_kernel(con
           }
         }
       }
-      if (!ok) {   // given up: what is under way lands before the CTA leaves
-        for (uint32_t i = it > R::stages ? it - R::stages : 0; i < it; ++i) bar_wait(full + 8 * (i % R::stages), i / R::stages & 1);
+      if (!ok) {   // what is under way lands before the CTA leaves
+        *gave_up = 1;
+        for (uint32_t i = it > R::stages ? it - R::stages : 0; i < it; ++i)
+          if (!bar_wait(full + 8 * (i % R::stages), i / R::stages & 1, ns)) break;
       }
     }
   } else if (warp == 1) {
@@ -122,12 +128,12 @@ __global__ void __launch_bounds__((Ring<BN>::threads), 1) product_f32_kernel(con
         const Tile t = tile_of(L, item, kbs);
         for (uint32_t kb = t.kb0; kb < t.kb1 && ok; ++ac) {
           const uint32_t end = min(kb + R::chunk, t.kb1), d = tmem + (ac & 1) * BN;
-          ok = bar_wait(acc_empty + 8 * (ac & 1), (ac >> 1 & 1) ^ 1);
+          ok = bar_wait(acc_empty + 8 * (ac & 1), (ac >> 1 & 1) ^ 1, ns);
           if (!ok) break;
           uint32_t accumulate = 0;
           for (; kb < end; ++kb, ++it) {
             const uint32_t s = it % R::stages;
-            ok = bar_wait(full + 8 * s, it / R::stages & 1) && bar_wait(apart + 8 * s, it / R::stages & 1);
+            ok = bar_wait(full + 8 * s, it / R::stages & 1, ns) && bar_wait(apart + 8 * s, it / R::stages & 1, ns);
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t a = tmem_a + s * R::a_cols;
@@ -146,6 +152,8 @@ __global__ void __launch_bounds__((Ring<BN>::threads), 1) product_f32_kernel(con
           if (ok) commit<1>(acc_full + 8 * (ac & 1));
         }
       }
+      if (!ok) *gave_up = 1;
+      commit<1>(drained);
     }
   } else if (warp < 2 + R::epi_warps) {
     const int ew = warp - 2;
@@ -163,7 +171,7 @@ __global__ void __launch_bounds__((Ring<BN>::threads), 1) product_f32_kernel(con
 #pragma unroll
         for (int i = 0; i < kBlock; ++i) sum[c][i] = 0.f;
       for (uint32_t kb = t.kb0; kb < t.kb1; kb += R::chunk, ++ac) {
-        if (ok) ok = bar_wait(acc_full + 8 * (ac & 1), ac >> 1 & 1);
+        if (ok && !bar_wait(acc_full + 8 * (ac & 1), ac >> 1 & 1, ns)) ok = false, *gave_up = 1;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
         for (int c = 0; c < kBlocks; ++c) {
@@ -210,8 +218,8 @@ __global__ void __launch_bounds__((Ring<BN>::threads), 1) product_f32_kernel(con
       const Tile t = tile_of(L, item, kbs);
       for (uint32_t kb = t.kb0; kb < t.kb1; ++kb, ++it) {
         const uint32_t s = it % R::stages;
-        ok = bar_wait(full + 8 * s, it / R::stages & 1);
-        if (!__all_sync(~0u, ok)) { ok = false; break; }
+        ok = bar_wait(full + 8 * s, it / R::stages & 1, ns);
+        if (!__all_sync(~0u, ok)) { ok = false, *gave_up = 1; break; }
         const unsigned char* a = sm + s * R::stage;
         uint32_t h[16], m[16], l[16];
         if (L.a_mn) {
@@ -244,6 +252,7 @@ __global__ void __launch_bounds__((Ring<BN>::threads), 1) product_f32_kernel(con
   __syncwarp();
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
+  if (warp == 1) drain(drained, *gave_up != 0, ns);
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   if (warp == 1) tmem_free<1>(tmem, 512);
 }
@@ -255,6 +264,7 @@ cudaError_t run(const MmaProduct& m, cudaStream_t s) {
   Launch L{};
   L.p = m.p;
   L.a_mn = m.a.mn; L.b_mn = m.b.mn;
+  L.waits = m.waits;
   L.splits = m.shape.splits;
   L.partial = m.partial; L.ld_partial = ((size_t)m.p.n + 3) / 4 * 4;
   L.tiles_m = (rows + 127) / 128;

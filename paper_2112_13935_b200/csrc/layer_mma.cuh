@@ -15,7 +15,6 @@ namespace {
 
 constexpr int kBlock = 16;         // columns that go through a warp's buffer at once
 
-constexpr unsigned long long kWaitNs = 4000000000ull;
 constexpr uint32_t kGroup = 16;     // tile rows that are walked together, so that their operands meet in L2
 
 struct Launch {
@@ -24,6 +23,7 @@ struct Launch {
   size_t ld_partial;
   uint32_t a_mn, b_mn;  // laid out across k
   uint32_t splits, tiles_m, tiles_n, idesc;
+  Waits waits;
 };
 
 // One lane of the warp, as the compiler knows: what only it does is kept in uniform registers, where tcgen05.mma takes its operands from.
@@ -34,8 +34,8 @@ __device__ __forceinline__ bool elect_one() {
 }
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count)); }
-// Waits, but not for ever: the longest wait there is, for the sums of a k of 2^31 in 32 parts, takes about half a second.
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
+// Waits, but not for ever (Waits says how long: the longest wait there is, for the sums of a k of 2^31 in 32 parts, takes about half a second).
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, unsigned long long most_ns) {
   unsigned long long from = 0;
   for (uint32_t i = 1;; ++i) {
     uint32_t ok;
@@ -46,7 +46,7 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
       unsigned long long now;
       asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
       if (!from) from = now;
-      if (now - from > kWaitNs) return false;
+      if (now - from > most_ns) return false;
     }
   }
 }
@@ -103,6 +103,21 @@ template <int CG>
 __device__ __forceinline__ void tmem_free(uint32_t at, uint32_t cols) {
   if (CG == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(cols));
   else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(cols));
+}
+// In front of the end of a CTA, by the warp that frees tensor memory, when all its roles are done: the products that were issued read shared
+// memory and write tensor memory until `drained` says that they are through, also where the roles that wait for sums have given up.  Then
+// copies whose barrier nobody waits for any more may be under way too; they land within some microseconds.
+__device__ __forceinline__ void drain(uint32_t drained, bool gave_up, unsigned long long most_ns) {
+  bar_wait(drained, 0, most_ns);
+  if (gave_up) {
+    unsigned long long from, now;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(from));
+    for (int i = 0; i < 1 << 20; ++i) {
+      asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
+      if (now - from > 100000) break;
+    }
+  }
+  __syncwarp();
 }
 // 16 columns of the warp's rows; they are there after tmem_wait.
 __device__ __forceinline__ void tmem_ld(uint32_t at, uint32_t (&r)[kBlock]) {

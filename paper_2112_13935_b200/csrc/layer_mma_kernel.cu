@@ -38,7 +38,10 @@ __global__ void __launch_bounds__((Ring<BN, CG>::threads), 1) product_mma_kernel
   unsigned char* sm = raw + (base - smem_u32(raw));
   float4* trans = reinterpret_cast<float4*>(sm + R::stages * R::stage);
   const uint32_t bars = base + R::stages * R::stage + R::trans;
-  const uint32_t full = bars, empty = bars + 8 * R::stages, acc_full = bars + 16 * R::stages, acc_empty = acc_full + 16, slot = acc_empty + 16;
+  const uint32_t full = bars, empty = bars + 8 * R::stages, acc_full = bars + 16 * R::stages, acc_empty = acc_full + 16, slot = acc_empty + 16,
+                 drained = slot + 8;
+  volatile uint32_t* gave_up = reinterpret_cast<uint32_t*>(sm + (drained + 8 - base));
+  const unsigned long long ns = L.waits.ns;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t rank = CG == 1 ? 0 : blockIdx.x % CG;   // of the pair; the even CTA issues for both
   const uint32_t first = blockIdx.x / CG, step = gridDim.x / CG;
@@ -54,6 +57,8 @@ __global__ void __launch_bounds__((Ring<BN, CG>::threads), 1) product_mma_kernel
       bar_init(acc_full + 8 * b, 1);
       bar_init(acc_empty + 8 * b, R::epi_warps * CG);
     }
+    bar_init(drained, 1);
+    *gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) tmem_alloc<CG>(slot, kCols);
@@ -75,7 +80,7 @@ __global__ void __launch_bounds__((Ring<BN, CG>::threads), 1) product_mma_kernel
         const int m0 = (int)(t.m * (128 * CG) + rank * 128), n0 = (int)(t.n * BN + rank * R::b_rows);
         for (uint32_t kb = t.kb0; kb < t.kb1; ++kb, ++it) {
           const uint32_t s = it % R::stages;
-          ok = bar_wait(empty + 8 * s, (it / R::stages & 1) ^ 1);
+          ok = bar_wait(empty + 8 * s, (it / R::stages & 1) ^ 1, ns) && (first || it < L.waits.stages);
           if (!ok) break;
           const uint32_t bar = CG == 1 ? full + 8 * s : in_cta(full + 8 * s, 0);
           if (rank == 0) bar_expect(full + 8 * s, R::stage * CG);
@@ -96,8 +101,10 @@ __global__ void __launch_bounds__((Ring<BN, CG>::threads), 1) product_mma_kernel
           }
         }
       }
-      if (!ok && rank == 0) {   // given up: what is under way lands before the CTA leaves
-        for (uint32_t i = it > R::stages ? it - R::stages : 0; i < it; ++i) bar_wait(full + 8 * (i % R::stages), i / R::stages & 1);
+      if (!ok) *gave_up = 1;
+      if (!ok && rank == 0) {   // what is under way lands before the CTA leaves
+        for (uint32_t i = it > R::stages ? it - R::stages : 0; i < it; ++i)
+          if (!bar_wait(full + 8 * (i % R::stages), i / R::stages & 1, ns)) break;
       }
     }
   } else if (warp == 1) {
@@ -108,13 +115,13 @@ __global__ void __launch_bounds__((Ring<BN, CG>::threads), 1) product_mma_kernel
       for (uint32_t item = first; item < items && ok; item += step) {
         const Tile t = tile_of(L, item, kbs);
         const uint32_t d = tmem + (ac & 1) * BN;
-        ok = bar_wait(acc_empty + 8 * (ac & 1), (ac >> 1 & 1) ^ 1);
+        ok = bar_wait(acc_empty + 8 * (ac & 1), (ac >> 1 & 1) ^ 1, ns);
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         uint32_t accumulate = 0;
         for (uint32_t kb = t.kb0; kb < t.kb1; ++kb, ++it) {
           const uint32_t s = it % R::stages;
-          ok = bar_wait(full + 8 * s, it / R::stages & 1);
+          ok = bar_wait(full + 8 * s, it / R::stages & 1, ns);
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const uint32_t at = base + s * R::stage;
@@ -129,6 +136,8 @@ __global__ void __launch_bounds__((Ring<BN, CG>::threads), 1) product_mma_kernel
         if (ok) commit<CG>(acc_full + 8 * (ac & 1));
         ++ac;
       }
+      if (!ok) *gave_up = 1;
+      commit<CG>(drained);
     }
   } else {
     const int ew = warp - 2, part = ew / 4;
@@ -143,7 +152,7 @@ __global__ void __launch_bounds__((Ring<BN, CG>::threads), 1) product_mma_kernel
       const uint32_t at = tmem + (lanes << 16) + part * R::cols;
       Ahead<Out> ahead;
       ahead.ask(L, lane, m0, n0);
-      if (ok) ok = bar_wait(acc_full + 8 * (ac & 1), ac >> 1 & 1);
+      if (ok && !bar_wait(acc_full + 8 * (ac & 1), ac >> 1 & 1, ns)) ok = false, *gave_up = 1;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
       for (int c = 0; c < kBlocks; ++c) {
@@ -174,6 +183,7 @@ __global__ void __launch_bounds__((Ring<BN, CG>::threads), 1) product_mma_kernel
   __syncwarp();
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
+  if (warp == 1) drain(drained, *gave_up != 0, ns);
   if (CG > 1) {   // neither CTA of a pair leaves while the other's products or barriers reach into it
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -188,6 +198,7 @@ cudaError_t run(const MmaProduct& m, cudaStream_t s) {
   Launch L{};
   L.p = m.p;
   L.a_mn = m.a.mn; L.b_mn = m.b.mn;
+  L.waits = m.waits;
   L.splits = m.shape.splits;
   L.partial = m.partial; L.ld_partial = ((size_t)m.p.n + 3) / 4 * 4;
   L.tiles_m = (m.p.m + 128 * CG - 1) / (128 * CG);

@@ -63,6 +63,12 @@ struct MmaShape {
   uint32_t pair;     // two CTAs share a tile
   uint32_t splits;   // parts k is split into
 };
+// How the tensor-core kernels wait for their barriers, and a failure that can be played: the copies of the first CTA (or pair) from its
+// `stages`-th stage on never come.
+struct Waits {
+  unsigned long long ns = 4000000000ull;
+  uint32_t stages = 0xffffffffu;
+};
 struct MmaProduct {
   Product p;         // m, n, k and the epilogue; a and b stand here:
   MmaOperand a, b;
@@ -70,6 +76,7 @@ struct MmaProduct {
   MmaShape shape;
   float* partial;    // mma_partial_floats() of workspace
   uint32_t swapped;  // fp32: a is B^T and b A^T, in parts; `shape` is that of n x m
+  Waits waits = {};
 };
 bool mma_takes(uint32_t type, uint32_t m, uint32_t n, uint32_t k);   // rather than the FMA kernel
 MmaShape mma_shape(uint32_t type, uint32_t m, uint32_t n, uint32_t k);

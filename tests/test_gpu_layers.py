@@ -552,3 +552,47 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for st, w in zip(states, want):
         assert all(torch.equal(w[k], st[3][k]) for k in w)
+
+
+# ---- a wait that gives up ------------------------------------------------------------------------------------------------
+
+# type, rows, n_in, n_out; stages a tile has, tiles of the first CTA (or pair), and the sums of a tile
+LOST = [("bf16", 2560, 640, 2304, 10, 2, 256 * 256),        # pairs of CTAs
+        ("f16", 1536, 320, 1536, 5, 1, 128 * 128),          # single CTAs
+        ("f16", 1024, 768, 1024, 6, 1, 128 * 128),          # ... and k in two parts
+        ("f32", 20000, 256, 128, 8, 2, 128 * 128),
+        ("f32", 8000, 512, 64, 8, 1, 128 * 64),             # 64 columns at a time, k in two parts
+        ("f32", 64, 1024, 4096, 8, 1, 128 * 64)]            # transposed, k in four
+
+
+@pytest.mark.parametrize("type,rows,n_in,n_out,stages,tiles,sums", LOST)
+def test_lost_copies_leave_nan_in_their_tiles_alone(type, rows, n_in, n_out, stages, tiles, sums):
+    t = lh.TYPES[type]
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    x, w = (torch.randn(n, generator=g, device="cuda").to(t) for n in ((rows, n_in), (n_in, n_out)))
+    plan = api.aet_dense(n_in, n_out, dtype=t)
+    ws = workspace(plan, rows, False)
+    want, y = torch.empty(rows, n_out, dtype=t, device="cuda"), torch.empty(rows, n_out, dtype=t, device="cuda")
+    api.aet_dense_forward(plan, x, w, None, want, workspace=ws)
+    assert not want.isnan().any()
+    for lost in (0, 1, stages - 1, stages, stages + 1, tiles * stages):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        api.aet_debug_dense_lost_copies(plan, x, w, y, ws, lost, 2000)
+        b.record()
+        torch.cuda.synchronize()
+        assert a.elapsed_time(b) < 2000
+        none = y.isnan()
+        assert int(none.sum()) == (tiles - min(tiles, lost // stages)) * sums, lost
+        assert torch.equal(y[~none], want[~none])
+        y.fill_(3.0)
+        api.aet_dense_forward(plan, x, w, None, y, workspace=ws)       # the next call is as ever
+        assert torch.equal(y, want)
+
+
+def test_lost_copies_refusals():
+    x = torch.zeros(4, 8, device="cuda")
+    for status, args in ((2, (0, 100)), (1, (0, 0)), (1, (0, 10 ** 6 + 1))):      # (a small product waits for nothing)
+        with pytest.raises(api.AetError) as e:
+            api.aet_debug_dense_lost_copies(api.aet_dense(8, 8), x, torch.zeros(8, 8, device="cuda"), x, None, *args)
+        assert e.value.status == status
