@@ -34,7 +34,7 @@ __device__ __forceinline__ bool elect_one() {
 }
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count)); }
-// Waits, but not for ever (Waits says how long: the longest wait there is, for the sums of a k of 2^31 in 32 parts, takes about half a second).
+// Waits, but not for ever (Waits says how long: the longest wait there is, for the sums of 2^17 of k, takes some 3 ms).
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, unsigned long long most_ns) {
   unsigned long long from = 0;
   for (uint32_t i = 1;; ++i) {

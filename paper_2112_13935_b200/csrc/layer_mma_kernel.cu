@@ -6,7 +6,7 @@
 // tensor memory.  Either operand may be laid out along k or across it: TMA brings 64 x 64 blocks either way and the matrix
 // descriptors say which, so that the gradients' transposed products read the tensors as they are.
 //
-// Few tiles and a long k: k is split, the parts' sums go to the workspace and a second kernel adds them up in their order.
+// Few tiles, or a very long k: k is split, the parts' sums go to the workspace and a second kernel adds them up in their order.
 //
 // Every wait is bounded; a role whose wait has given up stops issuing, and tiles that were not summed are stored as NaN.
 #include "layer_mma.cuh"
@@ -237,6 +237,7 @@ cudaError_t run(const MmaProduct& m, cudaStream_t s) {
 bool mma_takes(uint32_t type, uint32_t m, uint32_t n, uint32_t k) {
   return fma_volume(m, n, k) >= (type == kF32 ? 1ull << 27 : 1ull << 25) || k / fma_split(m, n, k) > 512;
 }
+constexpr uint64_t kMostBlocks = (1u << 17) / 64;
 MmaShape mma_shape(uint32_t type, uint32_t m, uint32_t n, uint32_t k) {
   MmaShape r{};
   const uint64_t pairs = (uint64_t)((m + 255) / 256) * ((n + 255) / 256);
@@ -248,6 +249,10 @@ MmaShape mma_shape(uint32_t type, uint32_t m, uint32_t n, uint32_t k) {
   const uint64_t least = type == kF32 ? 2 : 4;
   if (splits > kbs / least) splits = kbs / least;
   if (splits > 32) splits = 32;
+  // At most 2^17 of k in a sum: the tensor cores cut what they add, 16 of k at a time, so that a long sum of one sign falls behind (0.6 of 2^-24
+  // of it every time: 2.4 % over 2^22 rows, 19 % over 2^31 in 32 parts); over 2^17 it is 3e-4, well below a rounding to 16 bits.
+  const uint64_t need = (kbs + kMostBlocks - 1) / kMostBlocks;
+  if (splits < need) splits = need;
   r.splits = splits < 2 ? 1 : (uint32_t)splits;
   return r;
 }

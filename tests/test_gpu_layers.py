@@ -596,3 +596,23 @@ def test_lost_copies_refusals():
         with pytest.raises(api.AetError) as e:
             api.aet_debug_dense_lost_copies(api.aet_dense(8, 8), x, torch.zeros(8, 8, device="cuda"), x, None, *args)
         assert e.value.status == status
+
+
+@pytest.mark.parametrize("type,rows,n_in,n_out", [("bf16", 2 ** 26 + 5, 8, 8), ("f16", 2 ** 22 + 3, 1024, 2400), ("f32", 2 ** 26 + 5, 8, 8)])
+def test_weight_gradient_over_very_many_rows(type, rows, n_in, n_out):
+    """Terms of one sign, where every addition that cuts loses a little: at most 2^17 of k go into one sum in tensor memory, 16 at a time, and
+    each addition there loses less than 2^-23 of the sum; the parts are added up rounded to nearest (fp32: sums of 64 are)."""
+    t = lh.TYPES[type]
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    x, dy = (torch.empty(rows, n, dtype=t, device="cuda") for n in (n_in, n_out))
+    for m in (x, dy):
+        for part in m.split(1 << 22):
+            part.copy_(torch.rand(part.shape, generator=g, device="cuda") * 2 ** -6)
+    want = sum(a.double().t() @ b.double() for a, b in zip(x[:, :16].split(1 << 22), dy[:, :16].split(1 << 22)))
+    plan = api.aet_dense(n_in, n_out, dtype=t)
+    dw = torch.empty(n_in, n_out, dtype=t, device="cuda")
+    api.aet_dense_backward(plan, x, None, dy, dw=dw, workspace=workspace(plan, rows, True))
+    parts = -(-rows // 2 ** 17)
+    cut = (parts + (2 ** 17 / 64 if type == "f32" else 0)) * 2.0 ** -24 + (24 * 2.0 ** -23 if type == "f32" else 2 ** 17 / 16 * 2.0 ** -23)
+    off = float(((dw[:16, :16].double() - want) / want).abs().max())
+    assert off <= cut + lh.HALF_STEP[t]
