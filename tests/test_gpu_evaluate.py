@@ -159,3 +159,33 @@ def test_evaluation_of_rows_that_do_not_fit_the_model():
     conv = workloads.get_config("cfg7", n_clients=1)
     with api.Session(conv, [], None) as s:
         assert (api.aet_n_inputs(s.h), api.aet_n_classes(s.h)) == (784, 10)
+
+
+@pytest.mark.parametrize("dims", [(784, 10), (784, 128, 10)])
+def test_evaluation_of_a_whole_training_set(dims):
+    """60,000 rows of the 28x28 sets: the products that many rows take, ten columns among them, against 64 bits."""
+    cfg, s, r = session(dims, l2=1e-4)
+    x, y = rows_of(r, 60000, dims)
+    x, y = torch.as_tensor(x).cuda(), torch.as_tensor(y).cuda()
+    with s:
+        w = s.model()
+        grad = torch.empty(w.size, device="cuda")
+        loss, right = s.evaluate(x, y, gradient=grad)
+        z = torch.empty(60000, dims[-1], device="cuda")
+        api.aet_predict(s.h, 0, x, z)
+        leaf = torch.as_tensor(w.astype(np.float64)).cuda().requires_grad_()
+        a, at, norm = x.double(), 0, 0
+        for l, (i, o) in enumerate(zip(dims, dims[1:])):
+            m = leaf[at:at + i * o].view(i, o)
+            a, norm = a @ m + leaf[at + i * o:at + i * o + o], norm + (m * m).sum()
+            at += i * o + o
+            if l + 2 < len(dims):
+                a = torch.relu(a)
+        want = torch.nn.functional.cross_entropy(a, y.long()) + 0.5 * sim.f32(1e-4) * norm
+        want.backward()
+        assert abs(loss - float(want.detach())) <= 1e-6 * max(1.0, float(want.detach()))
+        # sums of 784 terms of a few tenths each: 800 2^-23 of their magnitudes at the very most
+        assert float((z - a).abs().max()) <= 800 * 2.0 ** -23 * 40
+        assert right == int((z.argmax(1) == y).sum())
+        g = leaf.grad
+        assert float((grad - g).abs().max()) <= 1e-5 * float(g.abs().max())

@@ -616,3 +616,37 @@ def test_weight_gradient_over_very_many_rows(type, rows, n_in, n_out):
     cut = (parts + (2 ** 17 / 64 if type == "f32" else 0)) * 2.0 ** -24 + (24 * 2.0 ** -23 if type == "f32" else 2 ** 17 / 16 * 2.0 ** -23)
     off = float(((dw[:16, :16].double() - want) / want).abs().max())
     assert off <= cut + lh.HALF_STEP[t]
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,n_in,n_out", [(3, 100, 300), (40, 70, 90), (300, 785, 300), (8000, 512, 64), (70, 1024, 4100), (2560, 640, 2304)])
+@pytest.mark.parametrize("value", [float("inf"), float("nan")])
+def test_infinities_stay_in_their_rows_and_columns(rows, n_in, n_out, type, value):
+    """Non-finite operands: their row or column of sums is not finite, every other sum as without them; every product kernel."""
+    t = lh.TYPES[type]
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    x, w, dy = (torch.randn(n, generator=g, device="cuda").to(t) for n in ((rows, n_in), (n_in, n_out), (rows, n_out)))
+    plan = api.aet_dense(n_in, n_out, dtype=t)
+
+    def run(x, w, dy):
+        y, dx, dw, db = (torch.empty(n, dtype=t, device="cuda") for n in ((rows, n_out), (rows, n_in), (n_in, n_out), (n_out,)))
+        api.aet_dense_forward(plan, x, w, None, y, workspace=workspace(plan, rows, False))
+        api.aet_dense_backward(plan, x, w, dy, dx=dx, dw=dw, db=db, workspace=workspace(plan, rows, True))
+        return y, dx, dw, db
+
+    want = run(x, w, dy)
+    assert all(v.isfinite().all() for v in want)
+    r, i, o = rows - 1, n_in // 2, n_out - 1
+    for name, at in (("x", (r, i)), ("w", (i, o)), ("dy", (r, o))):
+        m = dict(x=x.clone(), w=w.clone(), dy=dy.clone())
+        m[name][at] = value
+        got = run(**m)
+        hit = [torch.zeros_like(v, dtype=torch.bool) for v in want]
+        if name == "x":
+            hit[0][r], hit[2][i] = True, True
+        elif name == "w":
+            hit[0][:, o], hit[1][:, i] = True, True
+        else:
+            hit[1][r], hit[2][:, o], hit[3][o] = True, True, True
+        for v, u, h in zip(got, want, hit):
+            assert not v[h].isfinite().any() and torch.equal(v[~h], u[~h]), name
