@@ -95,9 +95,11 @@ def aet_set_global_model(h, w0, stream=None):
                                                _stream(stream)))
 
 
-def _kind(a, kind: str, what: str):
-    if str(a.dtype).rsplit(".", 1)[-1] != kind:
-        raise AetError(1, f"{what}: {a.dtype}, expected {kind}")
+def _kind(a, kind, what: str):
+    """Held to a type (or one of several)."""
+    kinds = (kind,) if isinstance(kind, str) else kind
+    if str(a.dtype).rsplit(".", 1)[-1] not in kinds:
+        raise AetError(1, f"{what}: {a.dtype}, expected {kinds[0]}")
 
 
 def _u32(v: int, what: str) -> int:
@@ -107,7 +109,7 @@ def _u32(v: int, what: str) -> int:
     return v
 
 
-def _rows(a, kind: str, n: int, width: int, what: str):
+def _rows(a, kind, n: int, width: int, what: str):
     """Held to its type and size, n rows of `width` values: the library gets an address and reads or writes that much behind it."""
     _kind(a, kind, what)
     _u32(n, "rows")
@@ -118,7 +120,7 @@ def _rows(a, kind: str, n: int, width: int, what: str):
 def aet_load_client_data(h, client: int, x, y, stream=None):
     n = x.shape[0]
     _rows(x, "float32", n, aet_n_inputs(h), "x")
-    _rows(y, "int32", n, 1, "y")
+    _rows(y, ("int32", "uint32"), n, 1, "y")          # (classes are not negative: the same bits)
     _check(h, _lib.load().aet_load_client_data(h, client, _ptr(x), _ptr(y), n, _stream(stream)))
 
 

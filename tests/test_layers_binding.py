@@ -90,7 +90,8 @@ def test_client_data_is_held_to_the_model(library):
     assert not library
     api.aet_load_client_data(None, 0, x.reshape(4, 3, 2, 2), y, stream=0)
     api.aet_load_client_data(None, 0, torch.from_numpy(x), torch.from_numpy(y), stream=0)
-    assert [c[4] for c in library] == [4, 4]
+    api.aet_load_client_data(None, 0, x, y.astype(np.uint32), stream=0)
+    assert [c[4] for c in library] == [4, 4, 4]
 
 
 def test_widths_of_no_handle():
