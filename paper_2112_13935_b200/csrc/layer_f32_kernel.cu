@@ -171,7 +171,10 @@ __global__ void __launch_bounds__((Ring<BN>::threads), 1) product_f32_kernel(con
 #pragma unroll
         for (int i = 0; i < kBlock; ++i) sum[c][i] = 0.f;
       for (uint32_t kb = t.kb0; kb < t.kb1; kb += R::chunk, ++ac) {
-        if (ok && !bar_wait(acc_full + 8 * (ac & 1), ac >> 1 & 1, ns)) ok = false, *gave_up = 1;
+        if (ok) {
+          ok = __all_sync(~0u, bar_wait(acc_full + 8 * (ac & 1), ac >> 1 & 1, ns));
+          if (!ok) *gave_up = 1;      // (from here on nothing is handed back either: the others may still take sums out)
+        }
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
         for (int c = 0; c < kBlocks; ++c) {
@@ -183,7 +186,7 @@ __global__ void __launch_bounds__((Ring<BN>::threads), 1) product_f32_kernel(con
         }
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         __syncwarp();
-        if (lane == 0) bar_arrive(acc_empty + 8 * (ac & 1));
+        if (lane == 0 && ok) bar_arrive(acc_empty + 8 * (ac & 1));
       }
 #pragma unroll
       for (int c = 0; c < kBlocks; ++c) {

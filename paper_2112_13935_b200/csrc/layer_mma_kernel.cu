@@ -152,7 +152,10 @@ __global__ void __launch_bounds__((Ring<BN, CG>::threads), 1) product_mma_kernel
       const uint32_t at = tmem + (lanes << 16) + part * R::cols;
       Ahead<Out> ahead;
       ahead.ask(L, lane, m0, n0);
-      if (ok && !bar_wait(acc_full + 8 * (ac & 1), ac >> 1 & 1, ns)) ok = false, *gave_up = 1;
+      if (ok) {
+        ok = __all_sync(~0u, bar_wait(acc_full + 8 * (ac & 1), ac >> 1 & 1, ns));
+        if (!ok) *gave_up = 1;      // (from here on nothing is handed back either: the others may still take sums out)
+      }
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
       for (int c = 0; c < kBlocks; ++c) {
@@ -165,7 +168,7 @@ __global__ void __launch_bounds__((Ring<BN, CG>::threads), 1) product_mma_kernel
         if (c == kBlocks - 1) {
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
           __syncwarp();
-          if (lane == 0) {
+          if (lane == 0 && ok) {
             if (CG == 1) bar_arrive(acc_empty + 8 * (ac & 1));
             else bar_arrive_pair(in_cta(acc_empty + 8 * (ac & 1), 0));
           }

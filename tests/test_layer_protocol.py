@@ -45,3 +45,12 @@ def test_every_wait_is_bounded():
     for name in KERNELS:
         for call in re.findall(r"bar_wait\((.*)$", kernel(name), re.M):
             assert re.search(r", ns\)", call), call
+
+
+@pytest.mark.parametrize("name", KERNELS)
+def test_a_warp_that_gave_up_hands_no_tensor_memory_back(name):
+    """A barrier counts arrivals, not who arrives: one warp running ahead would stand for another that still reads."""
+    k = kernel(name)
+    assert re.search(r"ok = __all_sync\(~0u, bar_wait\(acc_full", k)          # a warp gives up as a whole
+    given = re.findall(r"if \(lane == 0( && ok)?\)[^;]*acc_empty", k)
+    assert given and all(given), given
