@@ -454,8 +454,9 @@ aet_status aet_debug_dense_lost_copies(const aet_dense_desc* d, size_t rows, con
 /* Gradient: dz = dropout(dy) act'(pre), dx = dz W^T, dW = x^T dz, db = sum of dz over
  * the rows.  dx, dw, db may be null, x if dw is, w if dx is, pre if act is
  * AET_ACT_NONE.  The residual's gradient is dy itself.  Large products take dz
- * rounded to dtype (the tensor cores' operands), small ones in fp32.  Outputs overlap
- * nothing. */
+ * rounded to dtype (the tensor cores' operands), small ones in fp32: an fp16 dz over
+ * 65,504, which a large dropout factor can make of a dy, is infinite in a large one.
+ * Outputs overlap nothing. */
 aet_status aet_dense_backward(const aet_dense_desc* d, size_t rows, const void* x, const void* w,
                               const void* pre, const void* dy, void* dx, void* dw, void* db, void* workspace,
                               size_t workspace_bytes, void* cuda_stream);

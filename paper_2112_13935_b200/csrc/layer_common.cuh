@@ -107,7 +107,7 @@ __device__ __forceinline__ void load4(uint32_t type, const void* p, size_t at, b
 // Activations for values that are stored as T.  relu'(0) = 0; gelu is z Phi(z) by the error function; silu is z sigmoid(z).
 // 16-bit results take a shorter way: exponentials by ex2.approx, and Phi(z) = 1 - P(t) e^(-z^2/2) / 2 for z >= 0 with t = 1 / (1 + p |z| / sqrt 2)
 // and Hastings' polynomial P (Abramowitz and Stegun 7.1.26), which is within 1.5e-7 / 2 of Phi everywhere and shares its exponential with
-// the density that the slope needs.
+// the density that the slope needs.  (The quotient in sigmoid is 0 for a divisor over 2^126: silu is exactly 0 below -87.3, where it is 1e-36.)
 template <class T> __device__ __forceinline__ float sigmoid(float z) {
   return sizeof(T) == 4 ? __fdividef(1.f, 1.f + expf(-z)) : __fdividef(1.f, 1.f + __expf(-z));
 }

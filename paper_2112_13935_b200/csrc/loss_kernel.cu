@@ -4,9 +4,11 @@
 // Bound by memory: each logit is read once and each gradient written once.  A row stays with those who read it: 4 to 32 lanes of a warp
 // (short rows, several to a warp), a CTA, or a cluster of up to eight CTAs, in 16-byte pieces as they lie in memory (those of CTAs wait in
 // shared memory).  The maximum m comes first, over lanes and warps, then the sum of exp(z - m); the CTAs of a cluster join both by one
-// push into the others' shared memory; then the gradient is formed.  Three CTAs share an SM, so that one's loads run under another's
-// stores.  What a warp does once a row costs as much as ten pieces, so a thread takes sixteen: 8,192 rows of 65,536 bf16 logits 396 us
-// (5.2 TB/s), with eight pieces 492.  Rows too long for a cluster (1.6 MB) are read again, from L2 as far as they fit there.
+// push into the others' shared memory; then the gradient is formed.  Several CTAs share an SM, so that one's loads run under another's
+// stores.  A thread takes up to sixteen pieces, counted as if its row started anywhere, so that aligned rows of a power of two of logits
+// get one step more CTAs than they would need, which is about even: 8,192 rows of 65,536 bf16 logits, eight pieces a thread, 395 us in a graph
+// (5.4 TB/s), with sixteen 406; 16,384 rows of 32,768 381 and 375.  Rows too long for a cluster (1.6 MB) are read again, from L2 as far as
+// they fit there.
 // Rows may start at any element: the pieces are those of the 16-byte grid, and what they hold besides the row counts as -inf.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
@@ -359,7 +361,7 @@ cudaError_t lanes(const LossLaunch& p, cudaStream_t s) {
   const uint64_t ctas = (p.rows + kThreads / G - 1) / (kThreads / G), x = ctas < kMostX ? ctas : kMostX;
   return launch(loss_lanes_kernel<T, G, NV>, dim3((unsigned)x, (unsigned)((ctas + x - 1) / x)), kThreads, 0, 1, s, p);
 }
-constexpr uint64_t kPieces = 4096, kMostPieces = 13 * 1024;     // of a CTA: 64 KB, so that three share an SM; 208 KB
+constexpr uint64_t kPieces = 4096, kMostPieces = 13 * 1024;     // of a CTA: 64 KB, so that three and more share an SM; 208 KB
 
 template <class T, bool kOnce, int THREADS>
 cudaError_t ctas(const LossLaunch& p, uint32_t width, uint64_t pieces, cudaStream_t s) {

@@ -185,7 +185,7 @@ def test_evaluation_of_a_whole_training_set(dims):
         want.backward()
         assert abs(loss - float(want.detach())) <= 1e-6 * max(1.0, float(want.detach()))
         # sums of 784 terms of a few tenths each: 800 2^-23 of their magnitudes at the very most
-        assert float((z - a).abs().max()) <= 800 * 2.0 ** -23 * 40
+        assert float((z - a.detach()).abs().max()) <= 800 * 2.0 ** -23 * 40
         assert right == int((z.argmax(1) == y).sum())
         g = leaf.grad
         assert float((grad - g).abs().max()) <= 1e-5 * float(g.abs().max())
